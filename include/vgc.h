@@ -383,6 +383,92 @@ vgc_status vgc_pack_indices(const uint32_t *words, const uint32_t *nnz, uint32_t
 vgc_status vgc_unpack_indices(const uint8_t *packed, const uint32_t *nnz, uint32_t max_words, uint32_t *words,
                               uint32_t *dev_status, vgc_stream_t stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * (6) Activation checkpoints in 8 bits.  The squared sums of (1) need every layer's input until the
+ * backward pass; kept in 8 bits it takes a quarter of its fp32 bytes.  (No paper counterpart.)
+ *
+ * Blocks of 32 neighbouring features of a row share a power-of-two scale 2^(e-127): the smallest, 2^-126
+ * at least, under which the largest finite |x| of the block is at most 448.  Code: x / scale in e4m3 (sign,
+ * 4 exponent, 3 mantissa bits), nearest, ties to even; infinities and NaN become NaN.  The value a code stands
+ * for is code * scale: within 2^-4 |x| where |x| >= 2^-6 scale, within 2^-10 scale below.
+ *
+ * Layout, for any number of features: codes [rows][Cp] (Cp = features rounded up to 128; the padding's codes
+ * are 0), then the bytes e as [Cp/128][Rp][4] (Rp = rows rounded up to 128, of padding rows 0): the scales of 128
+ * neighbouring features of neighbouring rows lie together, as the products of (8) read them.
+ *
+ *   vgc_checkpoint_bytes   size of the buffer (0 when rows or features is 0 or negative)
+ *   vgc_checkpoint_store   x [rows][features] of `type` -> checkpoint (every byte of it is written)
+ *   vgc_checkpoint_load    the values the checkpoint stands for -> x [rows][features] of `type` (exact in both types
+ *                          but for their ends: below 2^-124 bf16 has fewer bits, and what rounded up to 2^128
+ *                          is infinity)
+ * x and checkpoint 16-byte aligned and separate; rows == 0 or features == 0: no-op, OK.  rows is below 2^31 - 128,
+ * features at most 2^24.
+ * ------------------------------------------------------------------------------------------- */
+typedef enum { VGC_FP32 = 0, VGC_BF16 = 1 } vgc_type;
+
+size_t vgc_checkpoint_bytes(int rows, int features);
+vgc_status vgc_checkpoint_store(const void *x, vgc_type type, int rows, int features, void *checkpoint,
+                                vgc_stream_t stream);
+vgc_status vgc_checkpoint_load(const void *checkpoint, int rows, int features, void *x, vgc_type type,
+                               vgc_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * (7) Layer norm, forward and backward, with the statistic of its gain and bias.  Per row r of x [rows][features]:
+ *   mean = sum x / features;  rstd = 1 / sqrt(sum (x - mean)^2 / features + eps);  xh = (x - mean) * rstd
+ *   y = xh * gamma + beta
+ * and on the way back, with dy = df/dy and w = dy * gamma:
+ *   dx = rstd * (w - mean(w) - xh * mean(w * xh))
+ *   g_gamma (+)= scale_g * sum_r dy * xh                     g_beta (+)= scale_g * sum_r dy
+ *   s_gamma (+)= scale_s * sum_e (sum_{r in e} dy * xh)^2    s_beta (+)= scale_s * sum_e (sum_{r in e} dy)^2
+ * where a sample e is `rows_per_example` neighbouring rows.  1: every row is a sample, the reading that vgc_sqgrad_conv
+ * takes of positions; T for sequences of T rows: the per-example statistic as Eq. 2 has it.  The paper treats no
+ * normalisation layers; g_* and s_* are the layer's slices of the buffers that vgc_compress takes as g and s.
+ *
+ *   x, y, dy, dx   `type`, [rows][features], 16-byte aligned.  y may be x; dx may be dy, or x.
+ *   gamma, beta    [features] fp32, 4-byte aligned; NULL: 1 and 0
+ *   mean, rstd     [rows] fp32: written by the forward call, read by the backward call
+ *   checkpoint     optional (NULL): the 8-bit checkpoint of y as it is stored, bit for bit what
+ *                  vgc_checkpoint_store(y) writes, for the linear layer that takes y (vgc_wgrad_checkpoint)
+ *   g_*, s_*       [features] fp32, 4-byte aligned, each optional (NULL); accumulate_g, accumulate_s: 0 written,
+ *                  1 added to with one fp32 addition
+ *   ws             at least vgc_layernorm_backward_workspace_bytes(...) bytes, 16-byte aligned
+ * Statistics and sums are fp32, column sums in a fixed order: the same inputs give the same bits.  rows == 0: the forward call
+ * is a no-op; the backward call's sums are empty (cleared, or left where accumulated).  features == 0: no-op, OK.
+ * features > VGC_NORM_MAX_FEATURES: VGC_ERR_UNSUPPORTED.  rows not a multiple of rows_per_example, eps negative or not finite,
+ * rows of 2^31 - 128 and more: VGC_ERR_INVALID_ARG.  NaN and infinities stay in their row of y and dx and reach the sums of
+ * their column (an infinity or NaN of x makes its whole row NaN).
+ * ------------------------------------------------------------------------------------------- */
+#define VGC_NORM_MAX_FEATURES 16384
+vgc_status vgc_layernorm(const void *x, vgc_type type, const float *gamma, const float *beta, int rows, int features,
+                         float eps, void *y, float *mean, float *rstd, void *checkpoint, vgc_stream_t stream);
+size_t vgc_layernorm_backward_workspace_bytes(int rows, int features, int rows_per_example);
+vgc_status vgc_layernorm_backward(const void *x, const void *dy, vgc_type type, const float *gamma, const float *mean,
+                                  const float *rstd, int rows, int features, int rows_per_example, float scale_g,
+                                  float scale_s, int accumulate_g, int accumulate_s, void *dx, float *g_gamma,
+                                  float *g_beta, float *s_gamma, float *s_beta, void *ws, size_t ws_bytes,
+                                  vgc_stream_t stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * (8) A linear layer's gradient and statistic in one pass over its input's checkpoint and its error:
+ *   g[o][i] (+)= scale_g * sum_r delta[r][o] * xq[r][i]
+ *   S[o][i] (+)= scale_s * sum_r delta[r][o]^2 * xq[r][i]^2        (every row a sample, as in vgc_sqgrad_conv)
+ * xq: the values of `checkpoint` ([rows][in], vgc_checkpoint_store or vgc_layernorm).
+ *
+ *   delta          `type`, [rows][out], 16-byte aligned
+ *   g, S           [out][in] fp32, 4-byte aligned; one of the two may be NULL; they do not overlap
+ *   accumulate_*   0: written  1: added to with one fp32 addition
+ *   ws             at least vgc_wgrad_checkpoint_workspace_bytes(...) bytes, 16-byte aligned; its first 32-bit word is the
+ *                  status word of (1): zeroed once by the caller, VGC_DEV_TIMEOUT if a wait gave up (results invalid)
+ * Every product enters exactly (bf16) or with 24 bits (fp32), sums are fp32: g within 2e-6 of the sum of the products'
+ * magnitudes, S within 1e-5 of the exact sum, for |xq| and |delta| that are 0 or within [2^-50, 2^50] and sums within
+ * fp32's range (squares and their low parts leave bf16's range beyond).  A row of delta or a column of xq with infinities or NaN gives infinities or NaN
+ * there.  rows == 0: the sums are empty (cleared, or left where accumulated).  in == 0 or out == 0: no-op, OK.
+ * ------------------------------------------------------------------------------------------- */
+size_t vgc_wgrad_checkpoint_workspace_bytes(int rows, int in, int out, vgc_type type);
+vgc_status vgc_wgrad_checkpoint(const void *checkpoint, const void *delta, vgc_type type, int rows, int in, int out,
+                                float scale_g, float scale_s, int accumulate_g, int accumulate_s, float *g, float *S,
+                                void *ws, size_t ws_bytes, vgc_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

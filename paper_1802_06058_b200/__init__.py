@@ -37,6 +37,9 @@ EXPORTS = [
     "vgc_compress_hybrid_workspace_bytes", "vgc_compress_hybrid", "vgc_decode_accumulate_hybrid",
     "vgc_decode_sum", "vgc_decode_sum_hybrid",
     "vgc_pack_bound_bytes", "vgc_pack_workspace_bytes", "vgc_pack_indices", "vgc_unpack_indices",
+    "vgc_checkpoint_bytes", "vgc_checkpoint_store", "vgc_checkpoint_load",
+    "vgc_layernorm", "vgc_layernorm_backward_workspace_bytes", "vgc_layernorm_backward",
+    "vgc_wgrad_checkpoint_workspace_bytes", "vgc_wgrad_checkpoint",
 ]
 
 
@@ -133,6 +136,18 @@ def load_library():
     lib.vgc_pack_indices.restype = i
     lib.vgc_unpack_indices.argtypes = [vp, vp, ctypes.c_uint32, vp, vp, vp]
     lib.vgc_unpack_indices.restype = i
+    lib.vgc_checkpoint_bytes.argtypes = [i, i]; lib.vgc_checkpoint_bytes.restype = sz
+    lib.vgc_checkpoint_store.argtypes = [vp, i, i, i, vp, vp]; lib.vgc_checkpoint_store.restype = i
+    lib.vgc_checkpoint_load.argtypes = [vp, i, i, vp, i, vp]; lib.vgc_checkpoint_load.restype = i
+    lib.vgc_layernorm.argtypes = [vp, i, vp, vp, i, i, f, vp, vp, vp, vp, vp]; lib.vgc_layernorm.restype = i
+    lib.vgc_layernorm_backward_workspace_bytes.argtypes = [i, i, i]
+    lib.vgc_layernorm_backward_workspace_bytes.restype = sz
+    lib.vgc_layernorm_backward.argtypes = [vp, vp, i, vp, vp, vp, i, i, i, f, f, i, i, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.vgc_layernorm_backward.restype = i
+    lib.vgc_wgrad_checkpoint_workspace_bytes.argtypes = [i, i, i, i]
+    lib.vgc_wgrad_checkpoint_workspace_bytes.restype = sz
+    lib.vgc_wgrad_checkpoint.argtypes = [vp, vp, i, i, i, i, f, f, i, i, vp, vp, vp, sz, vp]
+    lib.vgc_wgrad_checkpoint.restype = i
     _lib = lib
     return lib
 
@@ -404,6 +419,80 @@ def vgc_unpack_indices(packed, nnz, words, dev_status, stream=None):
     if st:
         _check(st, "vgc_unpack_indices")
     return words
+
+
+# ------------------------------------------------------------------------------------------ (6)
+VGC_FP32, VGC_BF16 = 0, 1
+
+
+def vgc_checkpoint_bytes(rows: int, features: int) -> int:
+    return load_library().vgc_checkpoint_bytes(int(rows), int(features))
+
+
+def vgc_checkpoint_store(x, checkpoint, stream=None):
+    """x [..., features] (fp32 or bf16) -> checkpoint, uint8 [vgc_checkpoint_bytes(rows, features)]: e4m3 codes with a
+    power-of-two scale per 32 features.  Rows are all dimensions but the last."""
+    st = (_native or load_native()).checkpoint_store(x, checkpoint, stream)
+    if st:
+        _check(st, "vgc_checkpoint_store")
+    return checkpoint
+
+
+def vgc_checkpoint_load(checkpoint, x, stream=None):
+    """The values a checkpoint stands for, written to x [..., features] (fp32 or bf16)."""
+    st = (_native or load_native()).checkpoint_load(checkpoint, x, stream)
+    if st:
+        _check(st, "vgc_checkpoint_load")
+    return x
+
+
+# ------------------------------------------------------------------------------------------ (7)
+VGC_NORM_MAX_FEATURES = 16384
+
+
+def vgc_layernorm(x, gamma, beta, eps: float, y, mean, rstd, checkpoint=None, stream=None):
+    """y = (x - mean) * rstd * gamma + beta over the last dimension of x (fp32 or bf16); mean, rstd fp32 [rows] are written
+    for the backward call.  gamma, beta fp32 or None; ``checkpoint``: also the 8-bit checkpoint of y."""
+    st = (_native or load_native()).layernorm(x, gamma, beta, eps, y, mean, rstd, checkpoint, stream)
+    if st:
+        _check(st, "vgc_layernorm")
+    return y
+
+
+def vgc_layernorm_backward_workspace_bytes(rows: int, features: int, rows_per_example: int = 1) -> int:
+    return load_library().vgc_layernorm_backward_workspace_bytes(int(rows), int(features), int(rows_per_example))
+
+
+def vgc_layernorm_backward(x, dy, gamma, mean, rstd, dx, g_gamma=None, g_beta=None, s_gamma=None, s_beta=None,
+                           scale_g: float = 1.0, scale_s: float = 1.0, accumulate_g: bool = False,
+                           accumulate_s: bool = False, rows_per_example: int = 1, ws=None, stream=None):
+    """dx, and for gain and bias the gradients g_* (+)= scale_g * sum and the sums of squared per-sample gradients
+    s_* (+)= scale_s * sum of squares; a sample is ``rows_per_example`` neighbouring rows."""
+    st = (_native or load_native()).layernorm_backward(x, dy, gamma, mean, rstd, dx, g_gamma, g_beta, s_gamma, s_beta, scale_g,
+                                                       scale_s, accumulate_g, accumulate_s, rows_per_example, ws, stream)
+    if st:
+        _check(st, "vgc_layernorm_backward")
+    return dx
+
+
+# ------------------------------------------------------------------------------------------ (8)
+def vgc_wgrad_checkpoint_workspace_bytes(rows: int, n_in: int, n_out: int, dtype=torch.bfloat16) -> int:
+    kind = {torch.float32: VGC_FP32, torch.bfloat16: VGC_BF16}.get(dtype)
+    if kind is None:
+        raise TypeError("delta must be torch.float32 or torch.bfloat16")
+    return load_library().vgc_wgrad_checkpoint_workspace_bytes(int(rows), int(n_in), int(n_out), kind)
+
+
+def vgc_wgrad_checkpoint(checkpoint, delta, g, S, scale_g: float = 1.0, scale_s: float = 1.0, accumulate_g: bool = False,
+                         accumulate_s: bool = False, ws=None, stream=None):
+    """From a linear layer's input checkpoint [rows][in] and its error delta [..., out] (fp32 or bf16): the gradient
+    g [out, in] (+)= scale_g * delta^T x and the statistic S [out, in] (+)= scale_s * (delta^2)^T x^2, in one pass.  One of
+    g and S may be None."""
+    st = (_native or load_native()).wgrad_checkpoint(checkpoint, delta, g, S, scale_g, scale_s, accumulate_g, accumulate_s, ws,
+                                                     stream)
+    if st:
+        _check(st, "vgc_wgrad_checkpoint")
+    return g if g is not None else S
 
 
 def vgc_step_host(layers, g_host, g_dev, s_dev, r, v, group_offsets, alpha, zeta, scale, out: MessageBuffers,

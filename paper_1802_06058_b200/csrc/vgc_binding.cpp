@@ -8,6 +8,7 @@
 // returned as integers and turned into exceptions there.  The GIL is released around the library call.
 #include <Python.h>
 
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -524,6 +525,145 @@ PyObject *step_host(Args a)
                            words_host, counters_host, wsg, wsgb, wsc, wscb, st));
 }
 
+// ---- activations: fp32 or bf16, gradients and statistics fp32.  These calls also refuse tensors that lie on another device than the
+// current one, whose streams they would be enqueued on.
+const at::Tensor &on_device(PyObject *o, const char *name)
+{
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda()) raise(PyExc_TypeError, "%s must be a CUDA tensor", name);
+    if (!t.is_contiguous()) raise(PyExc_ValueError, "%s must be contiguous", name);
+    if (t.device().index() != c10::cuda::current_device()) raise(PyExc_ValueError, "%s is not on the current device", name);
+    return t;
+}
+vgc_type type_of(const at::Tensor &t, const char *name)
+{
+    if (t.scalar_type() == at::kFloat) return VGC_FP32;
+    if (t.scalar_type() != at::kBFloat16) raise(PyExc_TypeError, "%s must be torch.float32 or torch.bfloat16", name);
+    return VGC_BF16;
+}
+// an activation matrix: rows of the last dimension
+struct Matrix {
+    void *p;
+    vgc_type type;
+    int64_t rows, features;
+};
+Matrix matrix(PyObject *o, const char *name)
+{
+    const at::Tensor &t = on_device(o, name);
+    Matrix m;
+    m.type = type_of(t, name);
+    if (t.dim() < 1) raise(PyExc_ValueError, "%s must have a last dimension of features", name);
+    m.features = t.size(-1);
+    m.rows = 1;
+    for (int64_t d = 0; d + 1 < t.dim(); ++d) m.rows *= t.size(d);
+    if (m.rows > INT32_MAX || m.features > INT32_MAX) raise(PyExc_ValueError, "%s is too large", name);
+    m.p = t.data_ptr();
+    return m;
+}
+void *same_matrix(PyObject *o, const char *name, const Matrix &as)
+{
+    const Matrix m = matrix(o, name);
+    if (m.type != as.type || m.rows != as.rows || m.features != as.features) raise(PyExc_ValueError, "%s differs in type or shape", name);
+    return m.p;
+}
+// fp32 values, `numel` of them; None: null
+float *vector(PyObject *o, const char *name, int64_t numel, bool optional)
+{
+    if (optional && o == Py_None) return nullptr;
+    const at::Tensor &t = on_device(o, name);
+    if (t.scalar_type() != at::kFloat) raise(PyExc_TypeError, "%s must be torch.float32", name);
+    if (t.numel() != numel) raise(PyExc_ValueError, "%s has another number of elements", name);
+    return static_cast<float *>(t.data_ptr());
+}
+void *checkpoint(PyObject *o, int64_t rows, int64_t features)
+{
+    const at::Tensor &t = on_device(o, "checkpoint");
+    if (t.scalar_type() != at::kByte) raise(PyExc_TypeError, "%s must be torch.uint8", "checkpoint");
+    if ((size_t)t.numel() != vgc_checkpoint_bytes((int)rows, (int)features))
+        raise(PyExc_ValueError, "%s is not of vgc_checkpoint_bytes(rows, features) bytes", "checkpoint");
+    return t.data_ptr();
+}
+void device_workspace(PyObject *o, void **p, size_t *bytes)
+{
+    if (o != Py_None) on_device(o, "workspace");
+    workspace(o, p, bytes);
+}
+
+// x, checkpoint, stream
+PyObject *checkpoint_store(Args a)
+{
+    const Matrix x = matrix(a[0], "x");
+    void *c = checkpoint(a[1], x.rows, x.features);
+    vgc_stream_t st = stream_of(a[2]);
+    VGC_CALL(vgc_checkpoint_store(x.p, x.type, (int)x.rows, (int)x.features, c, st));
+}
+
+// checkpoint, x, stream
+PyObject *checkpoint_load(Args a)
+{
+    const Matrix x = matrix(a[1], "x");
+    const void *c = checkpoint(a[0], x.rows, x.features);
+    vgc_stream_t st = stream_of(a[2]);
+    VGC_CALL(vgc_checkpoint_load(c, (int)x.rows, (int)x.features, x.p, x.type, st));
+}
+
+// x, gamma, beta, eps, y, mean, rstd, checkpoint, stream
+PyObject *layernorm(Args a)
+{
+    const Matrix x = matrix(a[0], "x");
+    const float *gamma = vector(a[1], "gamma", x.features, true), *beta = vector(a[2], "beta", x.features, true);
+    const float eps = (float)number(a[3]);
+    void *y = same_matrix(a[4], "y", x);
+    float *mean = vector(a[5], "mean", x.rows, false), *rstd = vector(a[6], "rstd", x.rows, false);
+    void *c = a[7] == Py_None ? nullptr : checkpoint(a[7], x.rows, x.features);
+    vgc_stream_t st = stream_of(a[8]);
+    VGC_CALL(vgc_layernorm(x.p, x.type, gamma, beta, (int)x.rows, (int)x.features, eps, y, mean, rstd, c, st));
+}
+
+// x, dy, gamma, mean, rstd, dx, g_gamma, g_beta, s_gamma, s_beta, scale_g, scale_s, accumulate_g, accumulate_s, rows_per_example,
+// ws, stream
+PyObject *layernorm_backward(Args a)
+{
+    const Matrix x = matrix(a[0], "x");
+    const void *dy = same_matrix(a[1], "dy", x);
+    const float *gamma = vector(a[2], "gamma", x.features, true);
+    const float *mean = vector(a[3], "mean", x.rows, false), *rstd = vector(a[4], "rstd", x.rows, false);
+    void *dx = same_matrix(a[5], "dx", x);
+    float *gg = vector(a[6], "g_gamma", x.features, true), *gb = vector(a[7], "g_beta", x.features, true);
+    float *sg = vector(a[8], "s_gamma", x.features, true), *sb = vector(a[9], "s_beta", x.features, true);
+    const float scale_g = (float)number(a[10]), scale_s = (float)number(a[11]);
+    const int acc_g = truth(a[12]), acc_s = truth(a[13]);
+    const long long per = integer(a[14]);
+    if (per < 1 || per > INT32_MAX || x.rows % per) raise(PyExc_ValueError, "rows must be a multiple of %s", "rows_per_example");
+    void *ws;
+    size_t wsb;
+    device_workspace(a[15], &ws, &wsb);
+    vgc_stream_t st = stream_of(a[16]);
+    VGC_CALL(vgc_layernorm_backward(x.p, dy, x.type, gamma, mean, rstd, (int)x.rows, (int)x.features, (int)per, scale_g, scale_s, acc_g,
+                                    acc_s, dx, gg, gb, sg, sb, ws, wsb, st));
+}
+
+// checkpoint, delta, g, S, scale_g, scale_s, accumulate_g, accumulate_s, ws, stream
+PyObject *wgrad_checkpoint(Args a)
+{
+    const Matrix d = matrix(a[1], "delta");
+    if (a[2] == Py_None && a[3] == Py_None) raise(PyExc_ValueError, "%s", "g and S are both None");
+    const at::Tensor &out = tensor(a[2] == Py_None ? a[3] : a[2], "g and S");
+    if (out.dim() != 2 || out.size(0) != d.features || out.size(1) > INT32_MAX)
+        raise(PyExc_ValueError, "%s must be [out][in], out the features of delta", "g and S");
+    const int64_t in = out.size(1), n = d.features * in;
+    float *g = vector(a[2], "g", n, true), *S = vector(a[3], "S", n, true);
+    if (g && S && (tensor(a[3], "S").dim() != 2 || tensor(a[3], "S").size(1) != in)) raise(PyExc_ValueError, "%s must be [out][in]", "S");
+    const void *c = checkpoint(a[0], d.rows, in);
+    const float scale_g = (float)number(a[4]), scale_s = (float)number(a[5]);
+    const int acc_g = truth(a[6]), acc_s = truth(a[7]);
+    void *ws;
+    size_t wsb;
+    device_workspace(a[8], &ws, &wsb);
+    vgc_stream_t st = stream_of(a[9]);
+    VGC_CALL(vgc_wgrad_checkpoint(c, d.p, d.type, (int)d.rows, (int)in, (int)d.features, scale_g, scale_s, acc_g, acc_s, g, S, ws, wsb, st));
+}
+
 // MessageBuffers, HybridMessageBuffers: the classes whose attributes are read directly
 PyObject *use_classes(Args a)
 {
@@ -570,6 +710,11 @@ PyMethodDef methods[] = {
     {"pack_indices", method<pack_indices, 7>(), METH_FASTCALL, nullptr},
     {"unpack_indices", method<unpack_indices, 5>(), METH_FASTCALL, nullptr},
     {"step_host", method<step_host, 16>(), METH_FASTCALL, nullptr},
+    {"checkpoint_store", method<checkpoint_store, 3>(), METH_FASTCALL, nullptr},
+    {"checkpoint_load", method<checkpoint_load, 3>(), METH_FASTCALL, nullptr},
+    {"layernorm", method<layernorm, 9>(), METH_FASTCALL, nullptr},
+    {"layernorm_backward", method<layernorm_backward, 17>(), METH_FASTCALL, nullptr},
+    {"wgrad_checkpoint", method<wgrad_checkpoint, 10>(), METH_FASTCALL, nullptr},
     {"use_classes", method<use_classes, 2>(), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -1,0 +1,257 @@
+// What the kernels share that pass over the rows of an activation matrix, fp32 or bf16: how a warp's lanes take 256 neighbouring
+// features of a row, and the 8-bit blocks of a checkpoint.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "vgc_common.cuh"
+
+namespace vgc {
+
+constexpr int kSeg = 256;           // features of a row that one warp takes: 8 per lane
+constexpr int kMaxRows = 2147483647 - 128;
+
+// Which features lane `lane` holds of a segment.  kVec (rows start on 16 bytes): 16-byte pieces, bf16 8 * lane + i, fp32
+// 128 * (i / 4) + 4 * lane + i % 4.  Otherwise single elements, neighbouring lanes next to one another: 32 * i + lane.
+template <class T, bool kVec>
+__device__ __forceinline__ int seg_col(int i, int lane)
+{
+    if (!kVec) return 32 * i + lane;
+    return sizeof(T) == 2 ? 8 * lane + i : 128 * (i >> 2) + 4 * lane + (i & 3);
+}
+
+// a lane's 8 features of a segment as they lie in memory
+template <class T> struct Raw;
+template <> struct Raw<float> { float v[8]; };
+template <> struct Raw<__nv_bfloat16> { uint32_t v[4]; };
+
+__device__ __forceinline__ uint4 ld_16(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ float ld_f(const float *p)
+{
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ uint32_t ld_h(const uint16_t *p)
+{
+    uint16_t v;
+    asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ void st_16(void *p, uint4 v)
+{
+    asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+// `seg`: the segment's first feature's address; `left`: features of the row from there on.  What lies past the row's end is 0.
+template <bool kVec>
+__device__ __forceinline__ void load_seg(const float *seg, int left, int lane, Raw<float> &r)
+{
+    if constexpr (kVec) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int c = 128 * j + 4 * lane;
+            const uint4 v = c < left ? ld_16(seg + c) : make_uint4(0, 0, 0, 0);
+            r.v[4 * j] = __uint_as_float(v.x); r.v[4 * j + 1] = __uint_as_float(v.y);
+            r.v[4 * j + 2] = __uint_as_float(v.z); r.v[4 * j + 3] = __uint_as_float(v.w);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = 32 * i + lane < left ? ld_f(seg + 32 * i + lane) : 0.f;
+    }
+}
+template <bool kVec>
+__device__ __forceinline__ void load_seg(const __nv_bfloat16 *seg, int left, int lane, Raw<__nv_bfloat16> &r)
+{
+    if constexpr (kVec) {
+        const uint4 v = 8 * lane < left ? ld_16(seg + 8 * lane) : make_uint4(0, 0, 0, 0);
+        r.v[0] = v.x; r.v[1] = v.y; r.v[2] = v.z; r.v[3] = v.w;
+    } else {
+        const uint16_t *const p = reinterpret_cast<const uint16_t *>(seg) + lane;
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] = 32 * i + lane < left ? ld_h(p + 32 * i) : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = h[2 * i] | h[2 * i + 1] << 16;
+    }
+}
+__device__ __forceinline__ float value(const Raw<float> &r, int i) { return r.v[i]; }
+__device__ __forceinline__ float value(const Raw<__nv_bfloat16> &r, int i)
+{
+    return __uint_as_float(i & 1 ? r.v[i >> 1] & 0xFFFF0000u : r.v[i >> 1] << 16);
+}
+// two values to the nearest bf16, the first in the low half
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b)
+{
+    uint32_t v;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(b), "f"(a));
+    return v;
+}
+__device__ __forceinline__ Raw<float> to_raw(const float (&v)[8], float)
+{
+    Raw<float> r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.v[i] = v[i];
+    return r;
+}
+__device__ __forceinline__ Raw<__nv_bfloat16> to_raw(const float (&v)[8], __nv_bfloat16)
+{
+    Raw<__nv_bfloat16> r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.v[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+    return r;
+}
+template <bool kVec>
+__device__ __forceinline__ void store_seg(float *seg, int left, int lane, const Raw<float> &r)
+{
+    if constexpr (kVec) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            if (128 * j + 4 * lane < left)
+                st_16(seg + 128 * j + 4 * lane, make_uint4(__float_as_uint(r.v[4 * j]), __float_as_uint(r.v[4 * j + 1]),
+                                                           __float_as_uint(r.v[4 * j + 2]), __float_as_uint(r.v[4 * j + 3])));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (32 * i + lane < left) seg[32 * i + lane] = r.v[i];
+    }
+}
+template <bool kVec>
+__device__ __forceinline__ void store_seg(__nv_bfloat16 *seg, int left, int lane, const Raw<__nv_bfloat16> &r)
+{
+    if constexpr (kVec) {
+        if (8 * lane < left) st_16(seg + 8 * lane, make_uint4(r.v[0], r.v[1], r.v[2], r.v[3]));
+    } else {
+        uint16_t *const p = reinterpret_cast<uint16_t *>(seg) + lane;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (32 * i + lane < left) p[32 * i] = (uint16_t)(r.v[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
+// ---- 8-bit checkpoints: codes [rows][wide] e4m3, scale exponents [wide / 128][tall][4] ---------------------------------------
+struct Checkpoint {
+    uint8_t *codes;
+    uint32_t *scales;                // four exponents a word
+    int wide, tall;                  // features rounded up to 128, rows to 128
+};
+inline int wide_of(int features) { return (int)round_up((size_t)features, 128); }
+inline int tall_of(int rows) { return (int)round_up((size_t)rows, 128); }
+inline Checkpoint checkpoint_at(void *p, int rows, int features)
+{
+    Checkpoint c;
+    c.wide = wide_of(features);
+    c.tall = tall_of(rows);
+    c.codes = static_cast<uint8_t *>(p);
+    c.scales = reinterpret_cast<uint32_t *>(c.codes + (size_t)rows * c.wide);
+    return c;
+}
+__device__ __forceinline__ uint32_t *scale_word(const Checkpoint &c, int row, int unit) { return c.scales + (size_t)unit * c.tall + row; }
+
+// |v|'s bits, 0 for infinities and NaN
+__device__ __forceinline__ uint32_t finite_magnitude(float v)
+{
+    const uint32_t b = __float_as_uint(v) & 0x7FFFFFFFu;
+    return b < 0x7F800000u ? b : 0u;
+}
+// the smallest exponent field e >= 1 with magnitude <= 448 * 2^(e - 127): 448 = 1.75 * 2^8, so e is the magnitude's exponent
+// less 8, one more where its mantissa is above 1.75
+__device__ __forceinline__ uint32_t scale_exponent(uint32_t magnitude)
+{
+    return (uint32_t)max((int)((magnitude + 0x1FFFFFu) >> 23) - 8, 1);
+}
+__device__ __forceinline__ float scale_of(uint32_t e) { return __uint_as_float(e << 23); }
+__device__ __forceinline__ float inverse_scale_of(uint32_t e) { return __uint_as_float((254u - e) << 23); }
+
+// two values / scale in e4m3, the first in the low byte.  v - v is 0, or NaN where v is infinite or NaN: those become NaN
+// (the conversion alone would make infinity 448).
+__device__ __forceinline__ uint32_t e4m3_pair(float a, float b, float inverse)
+{
+    uint16_t v;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(__fmaf_rn(b, inverse, b - b)), "f"(__fmaf_rn(a, inverse, a - a)));
+    return v;
+}
+// two codes as numbers (exact)
+__device__ __forceinline__ void e4m3_values(uint32_t pair, float &a, float &b)
+{
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)pair));
+    asm("{\n\t.reg .b16 l, u;\n\tmov.b32 {l, u}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, u;\n\t}" : "=f"(a), "=f"(b) : "r"(h));
+}
+
+// A segment's values into the checkpoint: all 32 lanes of the warp, features `first` ... of row `row` (first a multiple of 256).
+// Lanes past the row's end hold zeros, and write the padding's zero codes.
+template <class T, bool kVec>
+__device__ __forceinline__ void store_blocks(const Checkpoint &c, int row, int first, int lane, const Raw<T> &r)
+{
+    uint8_t *const codes = c.codes + (size_t)row * c.wide + first;
+    const int left = c.wide - first, unit = first >> 7;
+    if constexpr (kVec && sizeof(T) == 2) {               // a block is four lanes, 128 features sixteen
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, finite_magnitude(value(r, i)));
+        m = max(m, __shfl_xor_sync(~0u, m, 1));
+        m = max(m, __shfl_xor_sync(~0u, m, 2));
+        const uint32_t e = scale_exponent(m);
+        const float inverse = inverse_scale_of(e);
+        uint32_t word = e << (8 * ((lane >> 2) & 3));
+        word |= __shfl_xor_sync(~0u, word, 4);
+        word |= __shfl_xor_sync(~0u, word, 8);
+        if (8 * lane < left) {
+            uint2 q;
+            q.x = e4m3_pair(value(r, 0), value(r, 1), inverse) | e4m3_pair(value(r, 2), value(r, 3), inverse) << 16;
+            q.y = e4m3_pair(value(r, 4), value(r, 5), inverse) | e4m3_pair(value(r, 6), value(r, 7), inverse) << 16;
+            *reinterpret_cast<uint2 *>(codes + 8 * lane) = q;
+            if ((lane & 15) == 0) *scale_word(c, row, unit + (lane >> 4)) = word;
+        }
+    } else if constexpr (kVec) {                          // a block is eight lanes, 128 features the warp
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = max(m, finite_magnitude(value(r, 4 * j + i)));
+            m = max(m, __shfl_xor_sync(~0u, m, 1));
+            m = max(m, __shfl_xor_sync(~0u, m, 2));
+            m = max(m, __shfl_xor_sync(~0u, m, 4));
+            const uint32_t e = scale_exponent(m);
+            const float inverse = inverse_scale_of(e);
+            uint32_t word = e << (8 * (lane >> 3));
+            word |= __shfl_xor_sync(~0u, word, 8);
+            word |= __shfl_xor_sync(~0u, word, 16);
+            if (128 * j < left) {
+                *reinterpret_cast<uint32_t *>(codes + 128 * j + 4 * lane) =
+                    e4m3_pair(value(r, 4 * j), value(r, 4 * j + 1), inverse) | e4m3_pair(value(r, 4 * j + 2), value(r, 4 * j + 3), inverse) << 16;
+                if (lane == 0) *scale_word(c, row, unit + j) = word;
+            }
+        }
+    } else {                                              // a block is one element of every lane
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t word = 0;
+#pragma unroll
+            for (int i = 4 * j; i < 4 * j + 4; ++i) {
+                const uint32_t e = scale_exponent(__reduce_max_sync(~0u, finite_magnitude(value(r, i))));
+                word |= e << (8 * (i & 3));
+                if (32 * i < left) codes[32 * i + lane] = (uint8_t)e4m3_pair(value(r, i), 0.f, inverse_scale_of(e));
+            }
+            if (lane == 0 && 128 * j < left) *scale_word(c, row, unit + j) = word;
+        }
+    }
+}
+
+// The scales of the rows that pad the checkpoint to a multiple of 128: zeros.  Any number of threads, `id` of `n`.
+__device__ __forceinline__ void clear_row_padding(const Checkpoint &c, int rows, uint32_t id, uint32_t n)
+{
+    const uint32_t pad = (uint32_t)(c.tall - rows), words = pad * (uint32_t)(c.wide >> 7);      // < 128 * 2^17
+    for (uint32_t i = id; i < words; i += n) {
+        const uint32_t unit = i / pad;
+        c.scales[(size_t)unit * c.tall + rows + (i - unit * pad)] = 0;
+    }
+}
+
+}  // namespace vgc

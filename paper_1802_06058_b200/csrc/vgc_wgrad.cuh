@@ -1,0 +1,26 @@
+// Arguments that the kernels of a linear layer's gradient and statistic share.
+#pragma once
+
+#include "vgc_rowpass.cuh"
+
+namespace vgc {
+
+struct WgradArgs {
+    float *g, *S;                    // [out][in], either may be null
+    int rows, in, out;
+    float scale_g, scale_s;
+    int accumulate_g, accumulate_s;
+    __device__ __forceinline__ void write_one(float *to, float v, float scale, int accumulate) const
+    {
+        v = __fmul_rn(scale, v);
+        *to = accumulate ? __fadd_rn(ld_f(to), v) : v;
+    }
+    __device__ __forceinline__ void write(int o, int i, float vg, float vs) const
+    {
+        const size_t at = (size_t)o * in + i;
+        if (g) write_one(g + at, vg, scale_g, accumulate_g);
+        if (S) write_one(S + at, vs, scale_s, accumulate_s);
+    }
+};
+
+}  // namespace vgc
