@@ -83,6 +83,8 @@ vgc_status simt_as(const WgradArgs &p, const void *delta, const Checkpoint &c, c
     return VGC_OK;
 }
 
+bool on_cuda_cores(int rows, int in, int out) { return (double)rows * in * out <= 0; }
+
 bool wgrad_shape_ok(int rows, int in, int out)
 {
     return rows >= 0 && rows <= kMaxRows && in >= 0 && in <= (1 << 24) && out >= 0 && out <= (1 << 22) - kTile;
@@ -96,7 +98,7 @@ using namespace vgc;
 extern "C" size_t vgc_wgrad_checkpoint_workspace_bytes(int rows, int in, int out, vgc_type type)
 {
     if (!wgrad_shape_ok(rows, in, out) || rows == 0 || in == 0 || out == 0 || (type != VGC_FP32 && type != VGC_BF16)) return 0;
-    return 256;
+    return round_up(on_cuda_cores(rows, in, out) ? 256 : wgrad_tc_workspace_bytes(rows, in, out, type), 256);
 }
 
 extern "C" vgc_status vgc_wgrad_checkpoint(const void *checkpoint, const void *delta, vgc_type type, int rows, int in, int out,
@@ -118,5 +120,6 @@ extern "C" vgc_status vgc_wgrad_checkpoint(const void *checkpoint, const void *d
     if (!ws || !aligned16(ws) || ws_bytes < vgc_wgrad_checkpoint_workspace_bytes(rows, in, out, type)) return VGC_ERR_WORKSPACE;
     const Checkpoint c = checkpoint_at(const_cast<void *>(checkpoint), rows, in);
     WgradArgs p = {g, S, rows, in, out, scale_g, scale_s, accumulate_g, accumulate_s};
+    if (!on_cuda_cores(rows, in, out)) return wgrad_tc(p, delta, type, c, ws, st);
     return type == VGC_FP32 ? simt_as<float>(p, delta, c, st) : simt_as<__nv_bfloat16>(p, delta, c, st);
 }

@@ -23,4 +23,7 @@ struct WgradArgs {
     }
 };
 
+size_t wgrad_tc_workspace_bytes(int rows, int in, int out, vgc_type type);
+vgc_status wgrad_tc(const WgradArgs &p, const void *delta, vgc_type type, const Checkpoint &c, void *ws, cudaStream_t st);
+
 }  // namespace vgc

@@ -1,0 +1,561 @@
+// A linear layer's gradient and squared-gradient sums from its input's 8-bit checkpoint and its error, on the tensor cores:
+//
+//   g[o][i] = sum_r delta[r][o] xq[r][i]          S[o][i] = sum_r delta[r][o]^2 xq[r][i]^2
+//
+// A restored code xq has 4 significant bits and a power-of-two scale: it is exact in bf16, and so is its square (8 bits).  delta in bf16 is
+// an operand as it is; its square has 16 bits, the sum of two bf16 exactly (hi = bf16(d^2), lo = d^2 - hi, one multiplication and one
+// fused multiply-add on packed pairs).  So three bf16 products with fp32 accumulation give both results, and only the accumulation
+// rounds.  delta in fp32: three bf16 parts of delta and three of delta^2, 24 bits each, six products.
+//
+// One block makes 128 inputs x 128 outputs of both results from one reading of its operands, 32 rows a slice:
+//   warp 0        one thread: TMA loads (codes, their scales, delta) into the raw ring
+//   warp 1        one thread: tcgen05.mma, operands in shared memory, both with the reduction outermost (MN-major)
+//   warps 4-11    two groups of four on alternate slices: codes -> xq, xq^2; delta -> its squares' parts (and its own, fp32)
+//   warps 12-19   four for g, four for S: every 256 rows they take the accumulator out of tensor memory and add it to running fp32
+//                 sums in registers (the tensor core truncates as it accumulates, about 1.3e-8 of the sum an instruction: 4e-7 over a run of
+//                 32), two accumulators in turn; at the end they write the tile, a lane an input: rows of 128 bytes
+// The work is the sequence of all tiles' slices.  Where whole tiles fill the SMs evenly, blocks take whole tiles; otherwise
+// every block takes an equal stretch of the sequence, leaves the tiles it shares with its neighbours as partial sums, and
+// wgrad_combine adds those in the blocks' order.
+// Bound: the tensor pipe, three (six) products of 128 x 128 x 16 at 116 cycles each.
+#include "vgc_tc.cuh"
+#include "vgc_wgrad.cuh"
+
+namespace vgc {
+namespace wgrad {
+
+using namespace tc;
+
+constexpr int kTile = 128, kSlice = 32, kChunk = 8;                 // slices per run of an accumulator
+constexpr uint32_t kOperand = kSlice * kTile * 2;                   // 8 KB: a bf16 operand of one slice
+constexpr uint32_t kCodes = kSlice * kTile, kScales = kSlice * 4;
+constexpr int kFirstTransform = 4, kGroups = 2, kFirstEpilogue = kFirstTransform + 4 * kGroups, kThreads = 32 * (kFirstEpilogue + 8);
+constexpr int kRegsLaunch = 96, kRegsFew = 40, kRegsTransform = 56, kRegsEpilogue = 160;
+static_assert(128 * (kRegsFew + kGroups * kRegsTransform + 2 * kRegsEpilogue) <= kRegsLaunch * kThreads && kThreads * kRegsLaunch <= 65536,
+              "the shares come out of what the block was launched with");
+// kParts: bf16 parts of delta.  One: the raw tile is the operand.  Three (fp32): they stand behind xq and xq^2, then those of the square.
+// The ring's sizes are even: the slot's previous user is then the same group of transform warps.
+template <int kParts> struct Ring {
+    static constexpr int kRaw = kParts == 1 ? 6 : 4, kOp = kParts == 1 ? 4 : 2;
+    static constexpr int kSquareParts = kParts == 1 ? 2 : 3;
+    static constexpr uint32_t kDelta = kParts == 1 ? kOperand : 2 * kOperand;
+    static constexpr uint32_t kRawBytes = kDelta + kCodes + 1024;   // [delta][codes][scales]
+    static constexpr uint32_t kOpBytes = (2 + (kParts == 1 ? 0 : 3) + kSquareParts) * kOperand;
+    static constexpr uint32_t kOpBase = kRaw * kRawBytes;
+    static constexpr uint32_t kSmem = kOpBase + kOp * kOpBytes + 1024 /*align*/;
+    static_assert(kRaw % 2 == 0 && kOp % 2 == 0 && kRawBytes % 1024 == 0 && kSmem <= 232448, "");
+};
+
+struct Params {
+    WgradArgs out;
+    const uint32_t *scales;
+    uint32_t *status;
+    float *partial;                  // [2 * blocks][2][128 o][128 i]
+    long long total;                 // slices of all tiles
+    int slices, tiles_i, tiles_o, tall;
+    bool whole;                      // blocks take whole tiles, `gridDim.x` apart
+};
+constexpr size_t kPartial = (size_t)kTile * kTile;                  // floats of one result
+
+__host__ __device__ inline long long first_slice(long long total, int blocks, int b)
+{
+    return total / blocks * b + total % blocks * b / blocks;
+}
+// tiles in bands of eight tiles of inputs, so that blocks that run side by side share operands of both kinds
+__device__ __forceinline__ void tile_at(const Params &p, int t, int &i0, int &o0)
+{
+    const int band = t / (8 * p.tiles_o), in_band = t - band * 8 * p.tiles_o, wide = min(8, p.tiles_i - 8 * band);
+    const int o = in_band / wide;
+    i0 = (8 * band + in_band - o * wide) * kTile;
+    o0 = o * kTile;
+}
+// The stretches of tiles that a block works on, one after another.
+struct Walk {
+    long long at, end;
+    int slices, step, tile, s0, s1;
+    bool whole;
+    __device__ explicit Walk(const Params &p) : slices(p.slices), whole(p.whole)
+    {
+        if (whole) {
+            step = (int)gridDim.x;
+            tile = (int)blockIdx.x - step;
+            end = (long long)p.tiles_i * p.tiles_o;
+        } else {
+            at = first_slice(p.total, gridDim.x, blockIdx.x);
+            end = first_slice(p.total, gridDim.x, blockIdx.x + 1);
+        }
+    }
+    __device__ bool next()
+    {
+        if (whole) {
+            tile += step;
+            s0 = 0;
+            s1 = slices;
+            return tile < end;
+        }
+        if (at >= end) return false;
+        tile = (int)(at / slices);
+        s0 = (int)(at - (long long)tile * slices);
+        s1 = (int)min((long long)slices, s0 + end - at);
+        at += s1 - s0;
+        return true;
+    }
+};
+
+__device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tc_ld_32x16(uint32_t taddr, uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+template <int kRegs> __device__ __forceinline__ void regs_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+template <int kRegs> __device__ __forceinline__ void regs_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegs)); }
+
+// packed bf16: d * d to the nearest, and what that leaves of the exact square (8 more bits: exact)
+__device__ __forceinline__ uint32_t square_hi(uint32_t d)
+{
+    uint32_t v;
+    asm("mul.rn.bf16x2 %0, %1, %1;" : "=r"(v) : "r"(d));
+    return v;
+}
+__device__ __forceinline__ uint32_t square_lo(uint32_t d, uint32_t hi)
+{
+    uint32_t v;
+    asm("fma.rn.bf16x2 %0, %1, %1, %2;" : "=r"(v) : "r"(d), "r"(hi ^ 0x80008000u));
+    return v;
+}
+// two numbers as three bf16 parts: each the nearest to what the ones before leave (exact but for the last's rounding)
+__device__ __forceinline__ void split3(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l)
+{
+    h = bf16_pair(a, b);
+    a = __fsub_rn(a, __uint_as_float(h << 16));
+    b = __fsub_rn(b, __uint_as_float(h & 0xFFFF0000u));
+    m = bf16_pair(a, b);
+    a = __fsub_rn(a, __uint_as_float(m << 16));
+    b = __fsub_rn(b, __uint_as_float(m & 0xFFFF0000u));
+    l = bf16_pair(a, b);
+}
+
+// `left` values to places `pitch` bytes apart.  One address that moves: worked out ahead, 128 of them took the registers of the sums.
+template <bool kAccumulate>
+__device__ __forceinline__ void write_column(const float (&sum)[kTile], float *to, size_t pitch, int left, float scale)
+{
+    uint64_t at = reinterpret_cast<uint64_t>(to);
+#pragma unroll
+    for (int j = 0; j < kTile; ++j) {
+        float v = __fmul_rn(scale, sum[j]);
+        if (j < left) {
+            if (kAccumulate) v = __fadd_rn(ld_f(reinterpret_cast<const float *>(at)), v);
+            asm volatile("st.global.f32 [%0], %1;" ::"l"(at), "f"(v) : "memory");
+        }
+        asm volatile("add.u64 %0, %0, %1;" : "+l"(at) : "l"(pitch));
+    }
+}
+
+// Operand tiles: MN-major with the 128-byte swizzle.  Blocks of 64 columns, 4096 bytes apart; a row (of the reduction) takes 128
+// bytes of a block, its 16-byte unit u in place u ^ (row & 7).
+template <int kParts>
+__global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_d, const Params prm)
+{
+    using R = Ring<kParts>;
+    extern __shared__ uint8_t smem_raw_[];
+    __shared__ __align__(8) uint64_t bars[2 * R::kRaw + 2 * R::kOp + 5];
+    __shared__ uint32_t tmem_base_slot;
+    __shared__ volatile uint32_t abort_flag;
+
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t smem_base = (smem_u32(smem_raw_) + 1023u) & ~1023u;
+    uint8_t *const smem_gen = smem_raw_ + (smem_base - smem_u32(smem_raw_));
+    uint64_t *const raw_full = bars, *const raw_empty = raw_full + R::kRaw, *const op_full = raw_empty + R::kRaw, *const op_empty = op_full + R::kOp;
+    uint64_t *const acc_full = op_empty + R::kOp, *const acc_empty = acc_full + 2, *const drain = acc_empty + 2;
+
+    grid_release();
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int i = 0; i < R::kRaw; ++i) {
+            mbar_init(smem_u32(&raw_full[i]), 1);
+            mbar_init(smem_u32(&raw_empty[i]), 1);
+        }
+        for (int i = 0; i < R::kOp; ++i) {
+            mbar_init(smem_u32(&op_full[i]), 4);
+            mbar_init(smem_u32(&op_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&acc_full[i]), 1);
+            mbar_init(smem_u32(&acc_empty[i]), 8);
+        }
+        mbar_init(smem_u32(drain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        prefetch_map(&map_x);
+        prefetch_map(&map_d);
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = tmem_base_slot;
+    grid_wait();
+
+    Walk walk(prm);
+    if (warp < (uint32_t)kFirstTransform) {
+        regs_dec<kRegsFew>();
+        if (warp == 0 && lane == 0) {
+            // ================= TMA producer (one thread) =================
+            int it = 0;
+            bool ok = true;
+            while (ok && walk.next()) {
+                int i0, o0;
+                tile_at(prm, walk.tile, i0, o0);
+                const uint32_t *const scales = prm.scales + (size_t)(i0 >> 7) * prm.tall;
+                for (int s = walk.s0; s < walk.s1; ++s, ++it) {
+                    const int st = it % R::kRaw;
+                    if (!mbar_wait(smem_u32(&raw_empty[st]), ((uint32_t)(it / R::kRaw) & 1u) ^ 1u, &abort_flag, 32)) { ok = false; break; }
+                    const uint32_t full = smem_u32(&raw_full[st]), dst = smem_base + (uint32_t)st * R::kRawBytes;
+                    mbar_expect_tx(full, R::kDelta + kCodes + kScales);
+                    constexpr int kBox = kParts == 1 ? 64 : 32;           // columns of 128 bytes
+#pragma unroll
+                    for (int j = 0; j < kTile / kBox; ++j) tma_load_2d(dst + j * 4096, &map_d, full, o0 + kBox * j, s * kSlice);
+                    tma_load_2d(dst + R::kDelta, &map_x, full, i0, s * kSlice);
+                    bulk_load(dst + R::kDelta + kCodes, scales + s * kSlice, kScales, full);
+                }
+            }
+            if (abort_flag) {                            // loads already issued must land before the block may exit
+                for (int i = it > R::kRaw ? it - R::kRaw : 0; i < it; ++i)
+                    for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(&raw_full[i % R::kRaw]), (uint32_t)(i / R::kRaw) & 1u); ++n) {}
+            }
+        } else if (warp == 1 && lane == 0) {
+            // ================= MMA issuer (one thread) =================
+            const uint64_t desc0 = smem_desc(0, 4096u, 1024u, 2u);
+            auto desc = [&](uint32_t addr) { return desc0 | (uint64_t)((addr >> 4) & 0x3FFFu); };
+            const uint32_t idesc = instr_desc_bf16(kTile, kTile) | (1u << 15) | (1u << 16);
+            const bool want_g = prm.out.g != nullptr, want_s = prm.out.S != nullptr;
+            int it = 0, c = 0;
+            bool ok = true;
+            while (ok && walk.next()) {
+                for (int s0 = walk.s0; ok && s0 < walk.s1; s0 += kChunk, ++c) {
+                    const int b = c & 1;
+                    ok = mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(c >> 1) & 1u) ^ 1u, &abort_flag, 0);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t d_g = tmem_base + (uint32_t)b * 2 * kTile, d_s = d_g + kTile;
+                    const int s1 = min(walk.s1, s0 + kChunk);
+                    for (int s = s0; s < s1; ++s, ++it) {
+                        const int raw = it % R::kRaw, op = it % R::kOp;
+                        ok = mbar_wait(smem_u32(&op_full[op]), (uint32_t)(it / R::kOp) & 1u, &abort_flag, 0);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t ops = smem_base + R::kOpBase + (uint32_t)op * R::kOpBytes;
+                        const uint32_t delta = kParts == 1 ? smem_base + (uint32_t)raw * R::kRawBytes : ops + 2 * kOperand;
+                        const uint32_t squares = ops + (kParts == 1 ? 2 : 5) * kOperand;
+#pragma unroll
+                        for (int kk = 0; kk < kSlice / 16; ++kk) {
+                            const uint32_t more = s > s0 || kk > 0 ? 1u : 0u;
+                            const uint64_t x1 = desc(ops + kk * 2048), x2 = desc(ops + kOperand + kk * 2048);
+                            if (want_g) {
+#pragma unroll
+                                for (int j = 0; j < kParts; ++j) mma_bf16(d_g, x1, desc(delta + j * kOperand + kk * 2048), idesc, j > 0 ? 1u : more);
+                            }
+                            if (want_s) {
+#pragma unroll
+                                for (int j = 0; j < R::kSquareParts; ++j) mma_bf16(d_s, x2, desc(squares + j * kOperand + kk * 2048), idesc, j > 0 ? 1u : more);
+                            }
+                        }
+                        tc_commit(smem_u32(&raw_empty[raw]));
+                        tc_commit(smem_u32(&op_empty[op]));
+                    }
+                    if (ok) tc_commit(smem_u32(&acc_full[b]));
+                }
+            }
+            if (!ok) {                                   // MMAs already issued must retire before tensor memory is freed
+                tc_commit(smem_u32(drain));
+                for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(drain), 0); ++n) {}
+            }
+        }
+    } else if (warp < (uint32_t)kFirstEpilogue) {
+        // ================= transform =================
+        regs_dec<kRegsTransform>();
+        const int tt = (int)(threadIdx.x - 32 * kFirstTransform) & 127, group = (int)(warp - kFirstTransform) >> 2;
+        int total = 0;
+        while (walk.next()) total += walk.s1 - walk.s0;
+        for (int i = group; i < total; i += kGroups) {
+            const int raw = i % R::kRaw, op = i % R::kOp;
+            if (!mbar_wait(smem_u32(&op_empty[op]), ((uint32_t)(i / R::kOp) & 1u) ^ 1u, &abort_flag)) break;
+            if (!mbar_wait(smem_u32(&raw_full[raw]), (uint32_t)(i / R::kRaw) & 1u, &abort_flag)) break;
+            const uint8_t *const in = smem_gen + (uint32_t)raw * R::kRawBytes;
+            uint8_t *const ops = smem_gen + R::kOpBase + (uint32_t)op * R::kOpBytes;
+            // codes: 32 rows of eight 16-byte pieces, two a thread
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t k = (uint32_t)(tt >> 3) + 16 * u, piece = tt & 7;
+                const uint4 q = *reinterpret_cast<const uint4 *>(in + R::kDelta + k * kTile + 16 * piece);
+                const uint32_t scales = *reinterpret_cast<const uint32_t *>(in + R::kDelta + kCodes + 4 * k);
+                const float scale = scale_of(scales >> (8 * (piece >> 1)) & 255u);
+                const uint32_t codes[4] = {q.x, q.y, q.z, q.w};
+                uint32_t x1[8], x2[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    float a, b;
+                    e4m3_values(codes[j >> 1] >> (16 * (j & 1)), a, b);
+                    x1[j] = bf16_pair(a * scale, b * scale);
+                    x2[j] = square_hi(x1[j]);
+                }
+                // neighbouring lanes start with different halves, so that eight of them fill the banks
+                uint8_t *const row = ops + (piece >> 2) * 4096 + k * 128;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t half = h ^ (piece >> 2), place = ((2 * (piece & 3) + half) ^ (k & 7)) << 4;
+                    const uint4 v1 = half ? make_uint4(x1[4], x1[5], x1[6], x1[7]) : make_uint4(x1[0], x1[1], x1[2], x1[3]);
+                    const uint4 v2 = half ? make_uint4(x2[4], x2[5], x2[6], x2[7]) : make_uint4(x2[0], x2[1], x2[2], x2[3]);
+                    *reinterpret_cast<uint4 *>(row + place) = v1;
+                    *reinterpret_cast<uint4 *>(row + kOperand + place) = v2;
+                }
+            }
+            if constexpr (kParts == 1) {                 // 512 pieces of eight errors, each to the same place
+                uint8_t *const squares = ops + 2 * kOperand;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t at = 16 * (tt + 128 * u);
+                    const uint4 d = *reinterpret_cast<const uint4 *>(in + at);
+                    uint4 h, l;
+                    h.x = square_hi(d.x); h.y = square_hi(d.y); h.z = square_hi(d.z); h.w = square_hi(d.w);
+                    l.x = square_lo(d.x, h.x); l.y = square_lo(d.y, h.y); l.z = square_lo(d.z, h.z); l.w = square_lo(d.w, h.w);
+                    *reinterpret_cast<uint4 *>(squares + at) = h;
+                    *reinterpret_cast<uint4 *>(squares + kOperand + at) = l;
+                }
+            } else {                                     // raw: boxes of 32 columns, swizzled likewise
+                uint8_t *const parts = ops + 2 * kOperand;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const uint32_t n = (uint32_t)tt + 128 * u, k = (n >> 2) & 31, col8 = (n & 3) + 4 * (n >> 7);      // eight columns 8 * col8
+                    const uint8_t *const row = in + (n >> 7) * 4096 + k * 128;
+                    float v[8];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float4 f = *reinterpret_cast<const float4 *>(row + (((2 * (n & 3) + h) ^ (k & 7)) << 4));
+                        v[4 * h] = f.x; v[4 * h + 1] = f.y; v[4 * h + 2] = f.z; v[4 * h + 3] = f.w;
+                    }
+                    const uint32_t at = (col8 >> 3) * 4096 + k * 128 + (((col8 & 7) ^ (k & 7)) << 4);
+#pragma unroll
+                    for (int w = 0; w < 2; ++w) {
+                        uint32_t h[4], m[4], l[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float a = w ? __fmul_rn(v[2 * j], v[2 * j]) : v[2 * j], b = w ? __fmul_rn(v[2 * j + 1], v[2 * j + 1]) : v[2 * j + 1];
+                            split3(a, b, h[j], m[j], l[j]);
+                        }
+                        uint8_t *const to = parts + 3 * w * kOperand + at;
+                        *reinterpret_cast<uint4 *>(to) = make_uint4(h[0], h[1], h[2], h[3]);
+                        *reinterpret_cast<uint4 *>(to + kOperand) = make_uint4(m[0], m[1], m[2], m[3]);
+                        *reinterpret_cast<uint4 *>(to + 2 * kOperand) = make_uint4(l[0], l[1], l[2], l[3]);
+                    }
+                }
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&op_full[op]));
+        }
+    } else {
+        // ================= epilogue =================
+        regs_inc<kRegsEpilogue>();
+        const uint32_t quarter = warp & 3, which = (warp - kFirstEpilogue) >> 2;      // lanes of tensor memory; g or S
+        const bool wanted = which == 0 ? prm.out.g != nullptr : prm.out.S != nullptr;
+        const uint32_t taddr = tmem_base + ((quarter * 32u) << 16) + which * kTile;
+        int c = 0;
+        bool ok = true;
+        while (ok && walk.next()) {
+            float sum[kTile];                            // (from zeros: set by the first run instead, they went through local memory)
+#pragma unroll
+            for (int j = 0; j < kTile; ++j) sum[j] = 0.f;
+            for (int s0 = walk.s0; s0 < walk.s1; s0 += kChunk, ++c) {
+                const int b = c & 1;
+                ok = mbar_wait(smem_u32(&acc_full[b]), (uint32_t)(c >> 1) & 1u, &abort_flag, 32);
+                if (!ok) break;
+                tc_fence_after();
+                if (wanted) {
+#pragma unroll
+                    for (int j = 0; j < kTile / 16; ++j) {
+                        uint32_t r[16];
+                        tc_ld_32x16(taddr + (uint32_t)b * 2 * kTile + 16 * j, r);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) sum[16 * j + k] = __fadd_rn(sum[16 * j + k], __uint_as_float(r[k]));
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
+            }
+            if (!ok || !wanted) continue;
+            int i0, o0;
+            tile_at(prm, walk.tile, i0, o0);
+            const int i = (int)(quarter * 32 + lane);
+            if (walk.s1 - walk.s0 == walk.slices) {
+                if (i0 + i < prm.out.in) {
+                    float *const to = (which == 0 ? prm.out.g : prm.out.S) + (size_t)o0 * prm.out.in + i0 + i;
+                    const float scale = which == 0 ? prm.out.scale_g : prm.out.scale_s;
+                    const size_t pitch = (size_t)prm.out.in * sizeof(float);
+                    const int left = prm.out.out - o0;
+                    if (which == 0 ? prm.out.accumulate_g : prm.out.accumulate_s) write_column<true>(sum, to, pitch, left, scale);
+                    else write_column<false>(sum, to, pitch, left, scale);
+                }
+            } else {                                     // behind the tile's beginning: the block's first stretch; else its last
+                float *const to = prm.partial + ((size_t)(2 * blockIdx.x + (walk.s0 > 0 ? 0 : 1)) * 2 + which) * kPartial + i;
+                write_column<false>(sum, to, kTile * sizeof(float), kTile, 1.f);
+            }
+        }
+    }
+
+    // ---- common exit ----
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+    }
+    if (threadIdx.x == 0 && abort_flag) atomicOr(prm.status, VGC_DEV_TIMEOUT);
+}
+
+// The tiles that blocks share: blockIdx.x + 1 is the block whose first slice lies inside the tile, the first such block of the tile.
+// 256 threads take eight rows of outputs.
+__global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int blocks)
+{
+    grid_release();
+    grid_wait();
+    const int b = (int)blockIdx.x + 1;
+    const long long at = first_slice(prm.total, blocks, b);
+    const int tile = (int)(at / prm.slices);
+    const long long begin = (long long)tile * prm.slices, end = begin + prm.slices;
+    if (at == begin || first_slice(prm.total, blocks, b - 1) > begin) return;
+    int i0, o0;
+    tile_at(prm, tile, i0, o0);
+    const int i = threadIdx.x & 127;
+    for (int o = blockIdx.y * 8 + (threadIdx.x >> 7); o < (int)blockIdx.y * 8 + 8; o += 2) {
+        const float *at0 = prm.partial + ((size_t)(2 * (b - 1) + 1) * 2) * kPartial + o * kTile + i;
+        float vg = prm.out.g ? ld_f(at0) : 0.f, vs = prm.out.S ? ld_f(at0 + kPartial) : 0.f;
+        for (int k = b; k < blocks && first_slice(prm.total, blocks, k) < end; ++k) {
+            const float *const more = prm.partial + ((size_t)(2 * k) * 2) * kPartial + o * kTile + i;
+            if (prm.out.g) vg += ld_f(more);
+            if (prm.out.S) vs += ld_f(more + kPartial);
+        }
+        if (i0 + i < prm.out.in && o0 + o < prm.out.out) prm.out.write(o0 + o, i0 + i, vg, vs);
+    }
+}
+
+// delta with rows of `pitch` elements, zeros behind the last: what TMA can address where `out` is not a multiple of 16 bytes
+template <class T>
+__global__ void __launch_bounds__(256) wgrad_repack(const T *delta, T *to, int rows, int out, int pitch)
+{
+    grid_release();
+    grid_wait();
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x)
+        for (int c = threadIdx.x; c < pitch; c += 256) to[row * pitch + c] = c < out ? delta[row * out + c] : T(0.f);
+}
+
+struct Plan {
+    int slices, tiles_i, tiles_o, blocks, pitch;
+    bool whole;
+    size_t partial_bytes, repack_bytes;
+};
+Plan plan_of(int rows, int in, int out, vgc_type type)
+{
+    Plan p;
+    p.slices = (rows + kSlice - 1) / kSlice;
+    p.tiles_i = (in + kTile - 1) / kTile;
+    p.tiles_o = (out + kTile - 1) / kTile;
+    const long long tiles = (long long)p.tiles_i * p.tiles_o, total = tiles * p.slices;
+    // whole tiles where their last round costs at most a twentieth
+    const long long rounds = (tiles + kSmCount - 1) / kSmCount;
+    p.whole = tiles * 20 >= rounds * kSmCount * 19 || p.slices == 1;
+    if (p.whole) p.blocks = (int)((tiles + rounds - 1) / rounds);
+    else p.blocks = total < kSmCount ? (int)total : kSmCount;
+    p.partial_bytes = p.whole ? 0 : (size_t)p.blocks * 2 * 2 * kPartial * sizeof(float);
+    const int item = type == VGC_FP32 ? 4 : 2;
+    p.pitch = (int)round_up((size_t)out, 16 / item);
+    p.repack_bytes = p.pitch == out ? 0 : round_up((size_t)rows * p.pitch * item, 256);
+    return p;
+}
+
+bool encode(CUtensorMap *map, CUtensorMapDataType type, const void *base, cuuint64_t columns, cuuint64_t rows, cuuint64_t pitch_bytes,
+            cuuint32_t box_columns, CUtensorMapSwizzle swizzle)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[2] = {columns, rows}, strides[1] = {pitch_bytes};
+    const cuuint32_t box[2] = {box_columns, (cuuint32_t)kSlice}, ones[2] = {1, 1};
+    const CUresult rc = fn(map, type, 2, const_cast<void *>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (rc != CUDA_SUCCESS && debug_enabled()) fprintf(stderr, "vgc: tensor map encode failed with CUresult %d\n", (int)rc);
+    return rc == CUDA_SUCCESS;
+}
+
+template <int kParts, class T>
+vgc_status launch(const WgradArgs &args, const T *delta, const Checkpoint &c, void *ws, cudaStream_t st)
+{
+    const Plan plan = plan_of(args.rows, args.in, args.out, kParts == 1 ? VGC_BF16 : VGC_FP32);
+    if ((long long)plan.tiles_i * plan.tiles_o >= (1LL << 28)) return VGC_ERR_UNSUPPORTED;
+    char *const space = static_cast<char *>(ws);
+    if (plan.repack_bytes) {
+        T *const packed = reinterpret_cast<T *>(space + 256 + plan.partial_bytes);
+        VGC_CUDA_OK(launch_kernel(wgrad_repack<T>, dim3((unsigned)(args.rows < 8 * kSmCount ? args.rows : 8 * kSmCount)), dim3(256), 0, st, true, delta, packed,
+                                  args.rows, args.out, plan.pitch));
+        count_launch();
+        delta = packed;
+    }
+    CUtensorMap map_x, map_d;
+    if (!encode(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, c.codes, (cuuint64_t)c.wide, (cuuint64_t)args.rows, (cuuint64_t)c.wide, kTile, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !encode(&map_d, kParts == 1 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, delta, (cuuint64_t)plan.pitch, (cuuint64_t)args.rows,
+                (cuuint64_t)plan.pitch * sizeof(T), 128 / sizeof(T), CU_TENSOR_MAP_SWIZZLE_128B))
+        return VGC_ERR_CUDA;
+    Params p;
+    p.out = args;
+    p.scales = c.scales;
+    p.status = static_cast<uint32_t *>(ws);
+    p.partial = reinterpret_cast<float *>(space + 256);
+    p.slices = plan.slices; p.tiles_i = plan.tiles_i; p.tiles_o = plan.tiles_o; p.tall = c.tall; p.whole = plan.whole;
+    p.total = (long long)plan.tiles_i * plan.tiles_o * plan.slices;
+    const auto fn = wgrad_tiles<kParts>;
+    VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), Ring<kParts>::kSmem, kRegsLaunch));
+    VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks), dim3(kThreads), Ring<kParts>::kSmem, st, true, map_x, map_d, p));
+    count_launch();
+    if (!plan.whole && plan.blocks > 1) {
+        VGC_CUDA_OK(launch_kernel(wgrad_combine, dim3((unsigned)plan.blocks - 1, kTile / 8), dim3(256), 0, st, true, p, plan.blocks));
+        count_launch();
+    }
+    return VGC_OK;
+}
+
+}  // namespace wgrad
+
+size_t wgrad_tc_workspace_bytes(int rows, int in, int out, vgc_type type)
+{
+    const wgrad::Plan p = wgrad::plan_of(rows, in, out, type);
+    return 256 + p.partial_bytes + p.repack_bytes;
+}
+
+vgc_status wgrad_tc(const WgradArgs &p, const void *delta, vgc_type type, const Checkpoint &c, void *ws, cudaStream_t st)
+{
+    return type == VGC_FP32 ? wgrad::launch<3, float>(p, static_cast<const float *>(delta), c, ws, st)
+                            : wgrad::launch<1, __nv_bfloat16>(p, static_cast<const __nv_bfloat16 *>(delta), c, ws, st);
+}
+
+}  // namespace vgc
