@@ -36,14 +36,14 @@ static_assert(128 * (kRegsFew + kGroups * kRegsTransform + 2 * kRegsEpilogue) <=
 // kParts: bf16 parts of delta.  One: the raw tile is the operand.  Three (fp32): they stand behind xq and xq^2, then those of the square.
 // The ring's sizes are even: the slot's previous user is then the same group of transform warps.
 template <int kParts> struct Ring {
-    static constexpr int kRaw = kParts == 1 ? 6 : 4, kOp = kParts == 1 ? 4 : 2;
+    static constexpr int kRaw = kParts == 1 ? 8 : 4, kOp = kParts == 1 ? 4 : 2;
     static constexpr int kSquareParts = kParts == 1 ? 2 : 3;
     static constexpr uint32_t kDelta = kParts == 1 ? kOperand : 2 * kOperand;
-    static constexpr uint32_t kRawBytes = kDelta + kCodes + 1024;   // [delta][codes][scales]
+    static constexpr uint32_t kRawBytes = kDelta + kCodes;          // [delta][codes]; the slots' scales lie behind both rings
     static constexpr uint32_t kOpBytes = (2 + (kParts == 1 ? 0 : 3) + kSquareParts) * kOperand;
     static constexpr uint32_t kOpBase = kRaw * kRawBytes;
-    static constexpr uint32_t kSmem = kOpBase + kOp * kOpBytes + 1024 /*align*/;
-    static_assert(kRaw % 2 == 0 && kOp % 2 == 0 && kRawBytes % 1024 == 0 && kSmem <= 232448, "");
+    static constexpr uint32_t kScaleBase = kOpBase + kOp * kOpBytes, kSmem = kScaleBase + kRaw * kScales + 1024 /*align*/;
+    static_assert(kRaw % 2 == 0 && kOp % 2 == 0 && kRawBytes % 1024 == 0 && kSmem + 512 <= 232448, "");
 };
 
 struct Params {
@@ -120,6 +120,13 @@ __device__ __forceinline__ void tc_ld_32x16(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr)
         : "memory");
 }
+// one lane of a converged warp, the same one every time
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
 {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -138,8 +145,17 @@ __device__ __forceinline__ uint32_t square_hi(uint32_t d)
 __device__ __forceinline__ uint32_t square_lo(uint32_t d, uint32_t hi)
 {
     uint32_t v;
-    asm("fma.rn.bf16x2 %0, %1, %1, %2;" : "=r"(v) : "r"(d), "r"(hi ^ 0x80008000u));
+    asm("{\n\t.reg .b32 n;\n\tneg.bf16x2 n, %2;\n\tfma.rn.bf16x2 %0, %1, %1, n;\n\t}" : "=r"(v) : "r"(d), "r"(hi));
     return v;
+}
+// two codes (low half) times a scale (twice, as fp32 bits): bf16, exact
+__device__ __forceinline__ uint32_t restored_pair(uint32_t codes, uint64_t scale)
+{
+    float a, b;
+    e4m3_values(codes, a, b);
+    uint64_t v = (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a);
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(v) : "l"(scale));
+    return bf16_pair(__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32)));
 }
 // two numbers as three bf16 parts: each the nearest to what the ones before leave (exact but for the last's rounding)
 __device__ __forceinline__ void split3(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l)
@@ -180,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
     __shared__ uint32_t tmem_base_slot;
     __shared__ volatile uint32_t abort_flag;
 
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     const uint32_t smem_base = (smem_u32(smem_raw_) + 1023u) & ~1023u;
     uint8_t *const smem_gen = smem_raw_ + (smem_base - smem_u32(smem_raw_));
     uint64_t *const raw_full = bars, *const raw_empty = raw_full + R::kRaw, *const op_full = raw_empty + R::kRaw, *const op_empty = op_full + R::kOp;
@@ -219,8 +235,8 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
     Walk walk(prm);
     if (warp < (uint32_t)kFirstTransform) {
         regs_dec<kRegsFew>();
-        if (warp == 0 && lane == 0) {
-            // ================= TMA producer (one thread) =================
+        if (warp == 0) {
+            // ================= TMA producer =================
             int it = 0;
             bool ok = true;
             while (ok && walk.next()) {
@@ -231,20 +247,24 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                     const int st = it % R::kRaw;
                     if (!mbar_wait(smem_u32(&raw_empty[st]), ((uint32_t)(it / R::kRaw) & 1u) ^ 1u, &abort_flag, 32)) { ok = false; break; }
                     const uint32_t full = smem_u32(&raw_full[st]), dst = smem_base + (uint32_t)st * R::kRawBytes;
-                    mbar_expect_tx(full, R::kDelta + kCodes + kScales);
                     constexpr int kBox = kParts == 1 ? 64 : 32;           // columns of 128 bytes
+                    if (elect_one()) {
+                        mbar_expect_tx(full, R::kDelta + kCodes + kScales);
 #pragma unroll
-                    for (int j = 0; j < kTile / kBox; ++j) tma_load_2d(dst + j * 4096, &map_d, full, o0 + kBox * j, s * kSlice);
-                    tma_load_2d(dst + R::kDelta, &map_x, full, i0, s * kSlice);
-                    bulk_load(dst + R::kDelta + kCodes, scales + s * kSlice, kScales, full);
+                        for (int j = 0; j < kTile / kBox; ++j) tma_load_2d(dst + j * 4096, &map_d, full, o0 + kBox * j, s * kSlice);
+                        tma_load_2d(dst + R::kDelta, &map_x, full, i0, s * kSlice);
+                        bulk_load(smem_base + R::kScaleBase + (uint32_t)st * kScales, scales + s * kSlice, kScales, full);
+                    }
+                    __syncwarp();
                 }
             }
             if (abort_flag) {                            // loads already issued must land before the block may exit
                 for (int i = it > R::kRaw ? it - R::kRaw : 0; i < it; ++i)
                     for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(&raw_full[i % R::kRaw]), (uint32_t)(i / R::kRaw) & 1u); ++n) {}
             }
-        } else if (warp == 1 && lane == 0) {
-            // ================= MMA issuer (one thread) =================
+        } else if (warp == 1) {
+            // ================= MMA issuer =================
+            // (the warp stays together and one lane issues: the operands' descriptors are then uniform values)
             const uint64_t desc0 = smem_desc(0, 4096u, 1024u, 2u);
             auto desc = [&](uint32_t addr) { return desc0 | (uint64_t)((addr >> 4) & 0x3FFFu); };
             const uint32_t idesc = instr_desc_bf16(kTile, kTile) | (1u << 15) | (1u << 16);
@@ -267,6 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                         const uint32_t ops = smem_base + R::kOpBase + (uint32_t)op * R::kOpBytes;
                         const uint32_t delta = kParts == 1 ? smem_base + (uint32_t)raw * R::kRawBytes : ops + 2 * kOperand;
                         const uint32_t squares = ops + (kParts == 1 ? 2 : 5) * kOperand;
+                        if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < kSlice / 16; ++kk) {
                             const uint32_t more = s > s0 || kk > 0 ? 1u : 0u;
@@ -282,12 +303,15 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                         }
                         tc_commit(smem_u32(&raw_empty[raw]));
                         tc_commit(smem_u32(&op_empty[op]));
+                        if (s + 1 == s1) tc_commit(smem_u32(&acc_full[b]));
+                        }
+                        __syncwarp();
                     }
-                    if (ok) tc_commit(smem_u32(&acc_full[b]));
                 }
             }
             if (!ok) {                                   // MMAs already issued must retire before tensor memory is freed
-                tc_commit(smem_u32(drain));
+                if (elect_one()) tc_commit(smem_u32(drain));
+                __syncwarp();
                 for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(drain), 0); ++n) {}
             }
         }
@@ -303,31 +327,29 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
             if (!mbar_wait(smem_u32(&raw_full[raw]), (uint32_t)(i / R::kRaw) & 1u, &abort_flag)) break;
             const uint8_t *const in = smem_gen + (uint32_t)raw * R::kRawBytes;
             uint8_t *const ops = smem_gen + R::kOpBase + (uint32_t)op * R::kOpBytes;
-            // codes: 32 rows of eight 16-byte pieces, two a thread
+            // codes: 32 rows of eight 16-byte pieces, two a thread.  Lanes of the right 64 columns take their halves the other way round:
+            // eight lanes that store together then fill the banks.
+            const uint32_t piece = tt & 7, side = piece >> 2;
+            const uint8_t *const scales = smem_gen + R::kScaleBase + (uint32_t)raw * kScales + (piece >> 1);
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint32_t k = (uint32_t)(tt >> 3) + 16 * u, piece = tt & 7;
+                const uint32_t k = (uint32_t)(tt >> 3) + 16 * u;
                 const uint4 q = *reinterpret_cast<const uint4 *>(in + R::kDelta + k * kTile + 16 * piece);
-                const uint32_t scales = *reinterpret_cast<const uint32_t *>(in + R::kDelta + kCodes + 4 * k);
-                const float scale = scale_of(scales >> (8 * (piece >> 1)) & 255u);
-                const uint32_t codes[4] = {q.x, q.y, q.z, q.w};
-                uint32_t x1[8], x2[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    float a, b;
-                    e4m3_values(codes[j >> 1] >> (16 * (j & 1)), a, b);
-                    x1[j] = bf16_pair(a * scale, b * scale);
-                    x2[j] = square_hi(x1[j]);
-                }
-                // neighbouring lanes start with different halves, so that eight of them fill the banks
-                uint8_t *const row = ops + (piece >> 2) * 4096 + k * 128;
+                const uint32_t bits = (uint32_t)scales[4 * k] << 23;
+                const uint64_t scale = (uint64_t)bits << 32 | bits;
+                const uint32_t codes[4] = {side ? q.z : q.x, side ? q.w : q.y, side ? q.x : q.z, side ? q.y : q.w};
+                uint8_t *const row = ops + side * 4096 + k * 128;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const uint32_t half = h ^ (piece >> 2), place = ((2 * (piece & 3) + half) ^ (k & 7)) << 4;
-                    const uint4 v1 = half ? make_uint4(x1[4], x1[5], x1[6], x1[7]) : make_uint4(x1[0], x1[1], x1[2], x1[3]);
-                    const uint4 v2 = half ? make_uint4(x2[4], x2[5], x2[6], x2[7]) : make_uint4(x2[0], x2[1], x2[2], x2[3]);
-                    *reinterpret_cast<uint4 *>(row + place) = v1;
-                    *reinterpret_cast<uint4 *>(row + kOperand + place) = v2;
+                    uint32_t x1[4], x2[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        x1[j] = restored_pair(codes[2 * h + (j >> 1)] >> (16 * (j & 1)), scale);
+                        x2[j] = square_hi(x1[j]);
+                    }
+                    const uint32_t place = ((2 * (piece & 3) + (side ^ h)) ^ (k & 7)) << 4;
+                    *reinterpret_cast<uint4 *>(row + place) = make_uint4(x1[0], x1[1], x1[2], x1[3]);
+                    *reinterpret_cast<uint4 *>(row + kOperand + place) = make_uint4(x2[0], x2[1], x2[2], x2[3]);
                 }
             }
             if constexpr (kParts == 1) {                 // 512 pieces of eight errors, each to the same place
