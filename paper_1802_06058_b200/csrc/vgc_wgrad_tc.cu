@@ -7,17 +7,20 @@
 // fused multiply-add on packed pairs).  So three bf16 products with fp32 accumulation give both results, and only the accumulation
 // rounds.  delta in fp32: three bf16 parts of delta and three of delta^2, 24 bits each, six products.
 //
-// One block makes 128 inputs x 128 outputs of both results from one reading of its operands, 32 rows a slice:
+// Two blocks, a cluster, make 256 inputs x 128 outputs of both results from one reading of their operands, 32 rows a slice.  Each
+// prepares the operands of its 128 inputs and of 64 of the outputs; the products (cta_group::2) read both blocks' shared memory and
+// leave each block the accumulators of its inputs.  In every block
 //   warp 0        one thread: TMA loads (codes, their scales, delta) into the raw ring
-//   warp 1        one thread: tcgen05.mma, operands in shared memory, both with the reduction outermost (MN-major)
+//   warp 1        (of the first block) one thread: tcgen05.mma, operands in shared memory, both with the reduction outermost (MN-major)
 //   warps 4-11    two groups of four on alternate slices: codes -> xq, xq^2; delta -> its squares' parts (and its own, fp32)
 //   warps 12-19   four for g, four for S: every 256 rows they take the accumulator out of tensor memory and add it to running fp32
 //                 sums in registers (the tensor core truncates as it accumulates, about 1.3e-8 of the sum an instruction: 4e-7 over a run of
 //                 32), two accumulators in turn; at the end they write the tile, a lane an input: rows of 128 bytes
 // The work is the sequence of all tiles' slices.  Where whole tiles fill the SMs evenly, blocks take whole tiles; otherwise
-// every block takes an equal stretch of the sequence, leaves the tiles it shares with its neighbours as partial sums, and
-// wgrad_combine adds those in the blocks' order.
-// Bound: the tensor pipe, three (six) products of 128 x 128 x 16 at 116 cycles each.
+// every pair takes an equal stretch of the sequence, leaves the tiles it shares with its neighbours as partial sums, and
+// wgrad_combine adds those in the pairs' order.
+// Bound: shared memory and power.  A block's six products of a slice (bf16) take 384 cycles of the tensor pipe; their operands, 36 KB, the
+// transform's 32 KB and TMA's 8 KB take 608 at 128 bytes a cycle.  (Single blocks of 128 x 128: 48 + 44 + 12 KB, 832 cycles.)
 #include "vgc_tc.cuh"
 #include "vgc_wgrad.cuh"
 
@@ -26,8 +29,9 @@ namespace wgrad {
 
 using namespace tc;
 
-constexpr int kTile = 128, kSlice = 32, kChunk = 8;                 // slices per run of an accumulator
-constexpr uint32_t kOperand = kSlice * kTile * 2;                   // 8 KB: a bf16 operand of one slice
+constexpr int kTileI = 256, kTile = 128, kHalf = 64;                // inputs, outputs of a pair; 128 and 64 a block
+constexpr int kSlice = 32, kChunk = 8;                              // rows; slices per run of an accumulator
+constexpr uint32_t kOperand = kSlice * kTile * 2, kErrors = kSlice * kHalf * 2;      // 8 KB, 4 KB: a bf16 operand of one slice
 constexpr uint32_t kCodes = kSlice * kTile, kScales = kSlice * 4;
 constexpr int kFirstTransform = 4, kGroups = 2, kFirstEpilogue = kFirstTransform + 4 * kGroups, kThreads = 32 * (kFirstEpilogue + 8);
 constexpr int kRegsLaunch = 96, kRegsFew = 40, kRegsTransform = 56, kRegsEpilogue = 160;
@@ -36,11 +40,11 @@ static_assert(128 * (kRegsFew + kGroups * kRegsTransform + 2 * kRegsEpilogue) <=
 // kParts: bf16 parts of delta.  One: the raw tile is the operand.  Three (fp32): they stand behind xq and xq^2, then those of the square.
 // The ring's sizes are even: the slot's previous user is then the same group of transform warps.
 template <int kParts> struct Ring {
-    static constexpr int kRaw = kParts == 1 ? 8 : 4, kOp = kParts == 1 ? 4 : 2;
+    static constexpr int kRaw = kParts == 1 ? 10 : 4, kOp = kParts == 1 ? 6 : 4;
     static constexpr int kSquareParts = kParts == 1 ? 2 : 3;
-    static constexpr uint32_t kDelta = kParts == 1 ? kOperand : 2 * kOperand;
+    static constexpr uint32_t kDelta = kParts == 1 ? kErrors : 2 * kErrors;
     static constexpr uint32_t kRawBytes = kDelta + kCodes;          // [delta][codes]; the slots' scales lie behind both rings
-    static constexpr uint32_t kOpBytes = (2 + (kParts == 1 ? 0 : 3) + kSquareParts) * kOperand;
+    static constexpr uint32_t kOpBytes = 2 * kOperand + ((kParts == 1 ? 0 : 3) + kSquareParts) * kErrors;
     static constexpr uint32_t kOpBase = kRaw * kRawBytes;
     static constexpr uint32_t kScaleBase = kOpBase + kOp * kOpBytes, kSmem = kScaleBase + kRaw * kScales + 1024 /*align*/;
     static_assert(kRaw % 2 == 0 && kOp % 2 == 0 && kRawBytes % 1024 == 0 && kSmem + 512 <= 232448, "");
@@ -50,26 +54,26 @@ struct Params {
     WgradArgs out;
     const uint32_t *scales;
     uint32_t *status;
-    float *partial;                  // [2 * blocks][2][128 o][128 i]
+    float *partial;                  // [2 * pairs][2][128 o][256 i]
     long long total;                 // slices of all tiles
-    int slices, tiles_i, tiles_o, tall;
-    bool whole;                      // blocks take whole tiles, `gridDim.x` apart
+    int slices, tiles_i, tiles_o, wide, tall;
+    bool whole;                      // pairs take whole tiles, as many apart as there are pairs
 };
-constexpr size_t kPartial = (size_t)kTile * kTile;                  // floats of one result
+constexpr size_t kPartial = (size_t)kTileI * kTile;                 // floats of one result
 
-__host__ __device__ inline long long first_slice(long long total, int blocks, int b)
+__host__ __device__ inline long long first_slice(long long total, int pairs, int b)
 {
-    return total / blocks * b + total % blocks * b / blocks;
+    return total / pairs * b + total % pairs * b / pairs;
 }
 // tiles in bands of eight tiles of inputs, so that blocks that run side by side share operands of both kinds
 __device__ __forceinline__ void tile_at(const Params &p, int t, int &i0, int &o0)
 {
     const int band = t / (8 * p.tiles_o), in_band = t - band * 8 * p.tiles_o, wide = min(8, p.tiles_i - 8 * band);
     const int o = in_band / wide;
-    i0 = (8 * band + in_band - o * wide) * kTile;
+    i0 = (8 * band + in_band - o * wide) * kTileI;
     o0 = o * kTile;
 }
-// The stretches of tiles that a block works on, one after another.
+// The stretches of tiles that a pair works on, one after another.
 struct Walk {
     long long at, end;
     int slices, step, tile, s0, s1;
@@ -77,12 +81,12 @@ struct Walk {
     __device__ explicit Walk(const Params &p) : slices(p.slices), whole(p.whole)
     {
         if (whole) {
-            step = (int)gridDim.x;
-            tile = (int)blockIdx.x - step;
+            step = (int)gridDim.x >> 1;
+            tile = (int)(blockIdx.x >> 1) - step;
             end = (long long)p.tiles_i * p.tiles_o;
         } else {
-            at = first_slice(p.total, gridDim.x, blockIdx.x);
-            end = first_slice(p.total, gridDim.x, blockIdx.x + 1);
+            at = first_slice(p.total, gridDim.x >> 1, blockIdx.x >> 1);
+            end = first_slice(p.total, gridDim.x >> 1, (blockIdx.x >> 1) + 1);
         }
     }
     __device__ bool next()
@@ -107,9 +111,42 @@ __device__ __forceinline__ void mma_bf16(uint32_t d_tmem, uint64_t a_desc, uint6
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
+}
+// an arrival at a barrier of both blocks of the pair once the products issued so far are done
+__device__ __forceinline__ void commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+// an arrival at the first block's barrier, from either block
+__device__ __forceinline__ void arrive_first(uint32_t bar)
+{
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(at) : "r"(bar));
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(at) : "memory");
+}
+// mbar_wait for arrivals that come from both blocks
+__device__ __forceinline__ bool wait_pair(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag)
+{
+    for (uint32_t i = 0; i < kWaitLimit; ++i) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+        if (ok) return true;
+        if (i >= 4 && *abort_flag) return false;
+    }
+    *abort_flag = 1;
+    return false;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tc_ld_32x16(uint32_t taddr, uint32_t (&r)[16])
 {
@@ -185,10 +222,10 @@ __device__ __forceinline__ void write_column(const float (&sum)[kTile], float *t
     }
 }
 
-// Operand tiles: MN-major with the 128-byte swizzle.  Blocks of 64 columns, 4096 bytes apart; a row (of the reduction) takes 128
+// Operand tiles of one block: MN-major with the 128-byte swizzle.  Blocks of 64 columns, 4096 bytes apart; a row (of the reduction) takes 128
 // bytes of a block, its 16-byte unit u in place u ^ (row & 7).
 template <int kParts>
-__global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_d, const Params prm)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_d, const Params prm)
 {
     using R = Ring<kParts>;
     extern __shared__ uint8_t smem_raw_[];
@@ -196,7 +233,7 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
     __shared__ uint32_t tmem_base_slot;
     __shared__ volatile uint32_t abort_flag;
 
-    const uint32_t warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
+    const uint32_t warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, rank = blockIdx.x & 1;
     const uint32_t smem_base = (smem_u32(smem_raw_) + 1023u) & ~1023u;
     uint8_t *const smem_gen = smem_raw_ + (smem_base - smem_u32(smem_raw_));
     uint64_t *const raw_full = bars, *const raw_empty = raw_full + R::kRaw, *const op_full = raw_empty + R::kRaw, *const op_empty = op_full + R::kOp;
@@ -210,12 +247,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
             mbar_init(smem_u32(&raw_empty[i]), 1);
         }
         for (int i = 0; i < R::kOp; ++i) {
-            mbar_init(smem_u32(&op_full[i]), 4);
+            mbar_init(smem_u32(&op_full[i]), 8);             // of both blocks (the second's own stay unused)
             mbar_init(smem_u32(&op_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&acc_full[i]), 1);
-            mbar_init(smem_u32(&acc_empty[i]), 8);
+            mbar_init(smem_u32(&acc_empty[i]), 16);
         }
         mbar_init(smem_u32(drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -223,11 +260,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
         prefetch_map(&map_d);
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
+    cluster_sync();
     tc_fence_after();
     const uint32_t tmem_base = tmem_base_slot;
     grid_wait();
@@ -242,16 +280,19 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
             while (ok && walk.next()) {
                 int i0, o0;
                 tile_at(prm, walk.tile, i0, o0);
-                const uint32_t *const scales = prm.scales + (size_t)(i0 >> 7) * prm.tall;
+                i0 += (int)rank * kTile;
+                o0 += (int)rank * kHalf;
+                // inputs past the last: codes 0 by TMA, any scales
+                const uint32_t *const scales = prm.scales + (size_t)(i0 < prm.wide ? i0 >> 7 : 0) * prm.tall;
                 for (int s = walk.s0; s < walk.s1; ++s, ++it) {
                     const int st = it % R::kRaw;
-                    if (!mbar_wait(smem_u32(&raw_empty[st]), ((uint32_t)(it / R::kRaw) & 1u) ^ 1u, &abort_flag, 32)) { ok = false; break; }
+                    if (!mbar_wait(smem_u32(&raw_empty[st]), ((uint32_t)(it / R::kRaw) & 1u) ^ 1u, &abort_flag, 0)) { ok = false; break; }
                     const uint32_t full = smem_u32(&raw_full[st]), dst = smem_base + (uint32_t)st * R::kRawBytes;
                     constexpr int kBox = kParts == 1 ? 64 : 32;           // columns of 128 bytes
                     if (elect_one()) {
                         mbar_expect_tx(full, R::kDelta + kCodes + kScales);
 #pragma unroll
-                        for (int j = 0; j < kTile / kBox; ++j) tma_load_2d(dst + j * 4096, &map_d, full, o0 + kBox * j, s * kSlice);
+                        for (int j = 0; j < kHalf / kBox; ++j) tma_load_2d(dst + j * 4096, &map_d, full, o0 + kBox * j, s * kSlice);
                         tma_load_2d(dst + R::kDelta, &map_x, full, i0, s * kSlice);
                         bulk_load(smem_base + R::kScaleBase + (uint32_t)st * kScales, scales + s * kSlice, kScales, full);
                     }
@@ -262,31 +303,31 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                 for (int i = it > R::kRaw ? it - R::kRaw : 0; i < it; ++i)
                     for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(&raw_full[i % R::kRaw]), (uint32_t)(i / R::kRaw) & 1u); ++n) {}
             }
-        } else if (warp == 1) {
+        } else if (warp == 1 && rank == 0) {
             // ================= MMA issuer =================
             // (the warp stays together and one lane issues: the operands' descriptors are then uniform values)
             const uint64_t desc0 = smem_desc(0, 4096u, 1024u, 2u);
             auto desc = [&](uint32_t addr) { return desc0 | (uint64_t)((addr >> 4) & 0x3FFFu); };
-            const uint32_t idesc = instr_desc_bf16(kTile, kTile) | (1u << 15) | (1u << 16);
+            const uint32_t idesc = instr_desc_bf16(kTile, kTileI) | (1u << 15) | (1u << 16);
             const bool want_g = prm.out.g != nullptr, want_s = prm.out.S != nullptr;
             int it = 0, c = 0;
             bool ok = true;
             while (ok && walk.next()) {
                 for (int s0 = walk.s0; ok && s0 < walk.s1; s0 += kChunk, ++c) {
                     const int b = c & 1;
-                    ok = mbar_wait(smem_u32(&acc_empty[b]), ((uint32_t)(c >> 1) & 1u) ^ 1u, &abort_flag, 0);
+                    ok = wait_pair(smem_u32(&acc_empty[b]), ((uint32_t)(c >> 1) & 1u) ^ 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d_g = tmem_base + (uint32_t)b * 2 * kTile, d_s = d_g + kTile;
                     const int s1 = min(walk.s1, s0 + kChunk);
                     for (int s = s0; s < s1; ++s, ++it) {
                         const int raw = it % R::kRaw, op = it % R::kOp;
-                        ok = mbar_wait(smem_u32(&op_full[op]), (uint32_t)(it / R::kOp) & 1u, &abort_flag, 0);
+                        ok = wait_pair(smem_u32(&op_full[op]), (uint32_t)(it / R::kOp) & 1u, &abort_flag);
                         if (!ok) break;
                         tc_fence_after();
                         const uint32_t ops = smem_base + R::kOpBase + (uint32_t)op * R::kOpBytes;
                         const uint32_t delta = kParts == 1 ? smem_base + (uint32_t)raw * R::kRawBytes : ops + 2 * kOperand;
-                        const uint32_t squares = ops + (kParts == 1 ? 2 : 5) * kOperand;
+                        const uint32_t squares = ops + 2 * kOperand + (kParts == 1 ? 0 : 3) * kErrors;
                         if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < kSlice / 16; ++kk) {
@@ -294,23 +335,23 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                             const uint64_t x1 = desc(ops + kk * 2048), x2 = desc(ops + kOperand + kk * 2048);
                             if (want_g) {
 #pragma unroll
-                                for (int j = 0; j < kParts; ++j) mma_bf16(d_g, x1, desc(delta + j * kOperand + kk * 2048), idesc, j > 0 ? 1u : more);
+                                for (int j = 0; j < kParts; ++j) mma_bf16(d_g, x1, desc(delta + j * kErrors + kk * 2048), idesc, j > 0 ? 1u : more);
                             }
                             if (want_s) {
 #pragma unroll
-                                for (int j = 0; j < R::kSquareParts; ++j) mma_bf16(d_s, x2, desc(squares + j * kOperand + kk * 2048), idesc, j > 0 ? 1u : more);
+                                for (int j = 0; j < R::kSquareParts; ++j) mma_bf16(d_s, x2, desc(squares + j * kErrors + kk * 2048), idesc, j > 0 ? 1u : more);
                             }
                         }
-                        tc_commit(smem_u32(&raw_empty[raw]));
-                        tc_commit(smem_u32(&op_empty[op]));
-                        if (s + 1 == s1) tc_commit(smem_u32(&acc_full[b]));
+                        commit_pair(smem_u32(&raw_empty[raw]));
+                        commit_pair(smem_u32(&op_empty[op]));
+                        if (s + 1 == s1) commit_pair(smem_u32(&acc_full[b]));
                         }
                         __syncwarp();
                     }
                 }
             }
             if (!ok) {                                   // MMAs already issued must retire before tensor memory is freed
-                if (elect_one()) tc_commit(smem_u32(drain));
+                if (elect_one()) commit_pair(smem_u32(drain));
                 __syncwarp();
                 for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(drain), 0); ++n) {}
             }
@@ -323,8 +364,8 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
         while (walk.next()) total += walk.s1 - walk.s0;
         for (int i = group; i < total; i += kGroups) {
             const int raw = i % R::kRaw, op = i % R::kOp;
-            if (!mbar_wait(smem_u32(&op_empty[op]), ((uint32_t)(i / R::kOp) & 1u) ^ 1u, &abort_flag)) break;
-            if (!mbar_wait(smem_u32(&raw_full[raw]), (uint32_t)(i / R::kRaw) & 1u, &abort_flag)) break;
+            if (!mbar_wait(smem_u32(&op_empty[op]), ((uint32_t)(i / R::kOp) & 1u) ^ 1u, &abort_flag, 0)) break;
+            if (!mbar_wait(smem_u32(&raw_full[raw]), (uint32_t)(i / R::kRaw) & 1u, &abort_flag, 0)) break;
             const uint8_t *const in = smem_gen + (uint32_t)raw * R::kRawBytes;
             uint8_t *const ops = smem_gen + R::kOpBase + (uint32_t)op * R::kOpBytes;
             // codes: 32 rows of eight 16-byte pieces, two a thread.  Lanes of the right 64 columns take their halves the other way round:
@@ -352,31 +393,31 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                     *reinterpret_cast<uint4 *>(row + kOperand + place) = make_uint4(x2[0], x2[1], x2[2], x2[3]);
                 }
             }
-            if constexpr (kParts == 1) {                 // 512 pieces of eight errors, each to the same place
+            if constexpr (kParts == 1) {                 // 256 pieces of eight errors, each to the same place
                 uint8_t *const squares = ops + 2 * kOperand;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+                for (int u = 0; u < 2; ++u) {
                     const uint32_t at = 16 * (tt + 128 * u);
                     const uint4 d = *reinterpret_cast<const uint4 *>(in + at);
                     uint4 h, l;
                     h.x = square_hi(d.x); h.y = square_hi(d.y); h.z = square_hi(d.z); h.w = square_hi(d.w);
                     l.x = square_lo(d.x, h.x); l.y = square_lo(d.y, h.y); l.z = square_lo(d.z, h.z); l.w = square_lo(d.w, h.w);
                     *reinterpret_cast<uint4 *>(squares + at) = h;
-                    *reinterpret_cast<uint4 *>(squares + kOperand + at) = l;
+                    *reinterpret_cast<uint4 *>(squares + kErrors + at) = l;
                 }
             } else {                                     // raw: boxes of 32 columns, swizzled likewise
                 uint8_t *const parts = ops + 2 * kOperand;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const uint32_t n = (uint32_t)tt + 128 * u, k = (n >> 2) & 31, col8 = (n & 3) + 4 * (n >> 7);      // eight columns 8 * col8
-                    const uint8_t *const row = in + (n >> 7) * 4096 + k * 128;
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t n = (uint32_t)tt + 128 * u, k = (n >> 2) & 31, col8 = (n & 3) + 4 * u;            // eight columns from 8 * col8 on
+                    const uint8_t *const row = in + u * 4096 + k * 128;
                     float v[8];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const float4 f = *reinterpret_cast<const float4 *>(row + (((2 * (n & 3) + h) ^ (k & 7)) << 4));
                         v[4 * h] = f.x; v[4 * h + 1] = f.y; v[4 * h + 2] = f.z; v[4 * h + 3] = f.w;
                     }
-                    const uint32_t at = (col8 >> 3) * 4096 + k * 128 + (((col8 & 7) ^ (k & 7)) << 4);
+                    const uint32_t at = k * 128 + ((col8 ^ (k & 7)) << 4);
 #pragma unroll
                     for (int w = 0; w < 2; ++w) {
                         uint32_t h[4], m[4], l[4];
@@ -385,16 +426,16 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                             const float a = w ? __fmul_rn(v[2 * j], v[2 * j]) : v[2 * j], b = w ? __fmul_rn(v[2 * j + 1], v[2 * j + 1]) : v[2 * j + 1];
                             split3(a, b, h[j], m[j], l[j]);
                         }
-                        uint8_t *const to = parts + 3 * w * kOperand + at;
+                        uint8_t *const to = parts + 3 * w * kErrors + at;
                         *reinterpret_cast<uint4 *>(to) = make_uint4(h[0], h[1], h[2], h[3]);
-                        *reinterpret_cast<uint4 *>(to + kOperand) = make_uint4(m[0], m[1], m[2], m[3]);
-                        *reinterpret_cast<uint4 *>(to + 2 * kOperand) = make_uint4(l[0], l[1], l[2], l[3]);
+                        *reinterpret_cast<uint4 *>(to + kErrors) = make_uint4(m[0], m[1], m[2], m[3]);
+                        *reinterpret_cast<uint4 *>(to + 2 * kErrors) = make_uint4(l[0], l[1], l[2], l[3]);
                     }
                 }
             }
             fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&op_full[op]));
+            if (lane == 0) arrive_first(smem_u32(&op_full[op]));
         }
     } else {
         // ================= epilogue =================
@@ -425,12 +466,12 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&acc_empty[b]));
+                if (lane == 0) arrive_first(smem_u32(&acc_empty[b]));
             }
             if (!ok || !wanted) continue;
             int i0, o0;
             tile_at(prm, walk.tile, i0, o0);
-            const int i = (int)(quarter * 32 + lane);
+            const int i = (int)(rank * kTile + quarter * 32 + lane);
             if (walk.s1 - walk.s0 == walk.slices) {
                 if (i0 + i < prm.out.in) {
                     float *const to = (which == 0 ? prm.out.g : prm.out.S) + (size_t)o0 * prm.out.in + i0 + i;
@@ -440,9 +481,9 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
                     if (which == 0 ? prm.out.accumulate_g : prm.out.accumulate_s) write_column<true>(sum, to, pitch, left, scale);
                     else write_column<false>(sum, to, pitch, left, scale);
                 }
-            } else {                                     // behind the tile's beginning: the block's first stretch; else its last
-                float *const to = prm.partial + ((size_t)(2 * blockIdx.x + (walk.s0 > 0 ? 0 : 1)) * 2 + which) * kPartial + i;
-                write_column<false>(sum, to, kTile * sizeof(float), kTile, 1.f);
+            } else {                                     // behind the tile's beginning: the pair's first stretch; else its last
+                float *const to = prm.partial + ((size_t)(2 * (blockIdx.x >> 1) + (walk.s0 > 0 ? 0 : 1)) * 2 + which) * kPartial + i;
+                write_column<false>(sum, to, kTileI * sizeof(float), kTile, 1.f);
             }
         }
     }
@@ -450,36 +491,59 @@ __global__ void __launch_bounds__(kThreads, 1) wgrad_tiles(const __grid_constant
     // ---- common exit ----
     tc_fence_before();
     __syncthreads();
+    cluster_sync();                                      // the products read the other block's shared memory, too
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512u) : "memory");
     }
     if (threadIdx.x == 0 && abort_flag) atomicOr(prm.status, VGC_DEV_TIMEOUT);
 }
 
-// The tiles that blocks share: blockIdx.x + 1 is the block whose first slice lies inside the tile, the first such block of the tile.
-// 256 threads take eight rows of outputs.
-__global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int blocks)
+// The tiles that pairs share: blockIdx.x + 1 is the pair whose first slice lies inside the tile, the first such pair of the tile.
+// 256 threads take 16 outputs: four neighbouring inputs and four of the outputs each.
+constexpr int kCombineRows = 16;
+__global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int pairs)
 {
+    __shared__ int found[2];                                  // the tile, pairs that share it
     grid_release();
+    if (threadIdx.x == 0) {
+        const int b = (int)blockIdx.x + 1;
+        const long long at = first_slice(prm.total, pairs, b), tile = at / prm.slices, begin = tile * prm.slices;
+        int n = 0;
+        if (at > begin && first_slice(prm.total, pairs, b - 1) <= begin)
+            for (n = 1; b - 1 + n < pairs && first_slice(prm.total, pairs, b - 1 + n) < begin + prm.slices; ++n) {}
+        found[0] = (int)tile;
+        found[1] = n;
+    }
+    __syncthreads();
+    const int n = found[1];
+    if (n == 0) return;
     grid_wait();
-    const int b = (int)blockIdx.x + 1;
-    const long long at = first_slice(prm.total, blocks, b);
-    const int tile = (int)(at / prm.slices);
-    const long long begin = (long long)tile * prm.slices, end = begin + prm.slices;
-    if (at == begin || first_slice(prm.total, blocks, b - 1) > begin) return;
     int i0, o0;
-    tile_at(prm, tile, i0, o0);
-    const int i = threadIdx.x & 127;
-    for (int o = blockIdx.y * 8 + (threadIdx.x >> 7); o < (int)blockIdx.y * 8 + 8; o += 2) {
-        const float *at0 = prm.partial + ((size_t)(2 * (b - 1) + 1) * 2) * kPartial + o * kTile + i;
-        float vg = prm.out.g ? ld_f(at0) : 0.f, vs = prm.out.S ? ld_f(at0 + kPartial) : 0.f;
-        for (int k = b; k < blocks && first_slice(prm.total, blocks, k) < end; ++k) {
-            const float *const more = prm.partial + ((size_t)(2 * k) * 2) * kPartial + o * kTile + i;
-            if (prm.out.g) vg += ld_f(more);
-            if (prm.out.S) vs += ld_f(more + kPartial);
+    tile_at(prm, found[0], i0, o0);
+    const int i = (int)(threadIdx.x & 63) * 4, o = (int)(blockIdx.y * kCombineRows + (threadIdx.x >> 6) * 4);
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float *const out = which == 0 ? prm.out.g : prm.out.S;
+        if (!out) continue;
+        float sum[4][4];
+        for (int k = 0; k < n; ++k) {                         // the first pair's last stretch, the others' first
+            const float *const from = prm.partial + ((size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * 2 + which) * kPartial + o * kTileI + i;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const uint4 v = ld_16(from + r * kTileI);
+                const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) sum[r][c] = k == 0 ? f[c] : __fadd_rn(sum[r][c], f[c]);
+            }
         }
-        if (i0 + i < prm.out.in && o0 + o < prm.out.out) prm.out.write(o0 + o, i0 + i, vg, vs);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (i0 + i + c < prm.out.in && o0 + o + r < prm.out.out)
+                    prm.out.write_one(out + (size_t)(o0 + o + r) * prm.out.in + i0 + i + c, sum[r][c], which == 0 ? prm.out.scale_g : prm.out.scale_s,
+                                      which == 0 ? prm.out.accumulate_g : prm.out.accumulate_s);
     }
 }
 
@@ -494,7 +558,7 @@ __global__ void __launch_bounds__(256) wgrad_repack(const T *delta, T *to, int r
 }
 
 struct Plan {
-    int slices, tiles_i, tiles_o, blocks, pitch;
+    int slices, tiles_i, tiles_o, pairs, pitch;
     bool whole;
     size_t partial_bytes, repack_bytes;
 };
@@ -502,15 +566,16 @@ Plan plan_of(int rows, int in, int out, vgc_type type)
 {
     Plan p;
     p.slices = (rows + kSlice - 1) / kSlice;
-    p.tiles_i = (in + kTile - 1) / kTile;
+    p.tiles_i = (in + kTileI - 1) / kTileI;
     p.tiles_o = (out + kTile - 1) / kTile;
     const long long tiles = (long long)p.tiles_i * p.tiles_o, total = tiles * p.slices;
-    // whole tiles where their last round costs at most a twentieth
-    const long long rounds = (tiles + kSmCount - 1) / kSmCount;
-    p.whole = tiles * 20 >= rounds * kSmCount * 19 || p.slices == 1;
-    if (p.whole) p.blocks = (int)((tiles + rounds - 1) / rounds);
-    else p.blocks = total < kSmCount ? (int)total : kSmCount;
-    p.partial_bytes = p.whole ? 0 : (size_t)p.blocks * 2 * 2 * kPartial * sizeof(float);
+    // In slices, of about 0.35 us: what a tile costs beside its slices, and what the partial tiles and their combining cost
+    constexpr int kMost = kSmCount / 2, kPerTile = 8, kCut = 32;
+    const long long rounds = (tiles + kMost - 1) / kMost;
+    p.whole = rounds * (p.slices + kPerTile) <= (total + kMost - 1) / kMost + kPerTile * ((tiles + kMost - 1) / kMost) + kCut;
+    if (p.whole) p.pairs = (int)((tiles + rounds - 1) / rounds);
+    else p.pairs = total < kMost ? (int)total : kMost;
+    p.partial_bytes = p.whole ? 0 : (size_t)p.pairs * 2 * 2 * kPartial * sizeof(float);
     const int item = type == VGC_FP32 ? 4 : 2;
     p.pitch = (int)round_up((size_t)out, 16 / item);
     p.repack_bytes = p.pitch == out ? 0 : round_up((size_t)rows * p.pitch * item, 256);
@@ -553,14 +618,14 @@ vgc_status launch(const WgradArgs &args, const T *delta, const Checkpoint &c, vo
     p.scales = c.scales;
     p.status = static_cast<uint32_t *>(ws);
     p.partial = reinterpret_cast<float *>(space + 256);
-    p.slices = plan.slices; p.tiles_i = plan.tiles_i; p.tiles_o = plan.tiles_o; p.tall = c.tall; p.whole = plan.whole;
+    p.slices = plan.slices; p.tiles_i = plan.tiles_i; p.tiles_o = plan.tiles_o; p.wide = c.wide; p.tall = c.tall; p.whole = plan.whole;
     p.total = (long long)plan.tiles_i * plan.tiles_o * plan.slices;
     const auto fn = wgrad_tiles<kParts>;
     VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), Ring<kParts>::kSmem, kRegsLaunch));
-    VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks), dim3(kThreads), Ring<kParts>::kSmem, st, true, map_x, map_d, p));
+    VGC_CUDA_OK(launch_kernel(fn, dim3(2u * (unsigned)plan.pairs), dim3(kThreads), Ring<kParts>::kSmem, st, true, map_x, map_d, p));
     count_launch();
-    if (!plan.whole && plan.blocks > 1) {
-        VGC_CUDA_OK(launch_kernel(wgrad_combine, dim3((unsigned)plan.blocks - 1, kTile / 8), dim3(256), 0, st, true, p, plan.blocks));
+    if (!plan.whole && plan.pairs > 1) {
+        VGC_CUDA_OK(launch_kernel(wgrad_combine, dim3((unsigned)plan.pairs - 1, kTile / kCombineRows), dim3(256), 0, st, true, p, plan.pairs));
         count_launch();
     }
     return VGC_OK;
