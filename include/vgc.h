@@ -460,8 +460,8 @@ vgc_status vgc_layernorm_backward(const void *x, const void *dy, vgc_type type, 
  *   ws             at least vgc_wgrad_checkpoint_workspace_bytes(...) bytes, 16-byte aligned; its first 32-bit word is the
  *                  status word of (1): zeroed once by the caller, VGC_DEV_TIMEOUT if a wait gave up (results invalid)
  * Every product enters exactly (bf16) or with 24 bits (fp32), sums are fp32: g within 2e-6 of the sum of the products'
- * magnitudes, S within 1e-5 of the exact sum, for |xq| and |delta| that are 0 or within [2^-50, 2^50] and sums within
- * fp32's range (squares and their low parts leave bf16's range beyond).  A row of delta or a column of xq with infinities or NaN gives infinities or NaN
+ * magnitudes, S within 1e-5 of the exact sum, for |xq| and |delta| that are 0 or within [2^-50, 2^50] and sums of
+ * magnitudes below 2^127 (squares and their low parts leave bf16's range beyond).  A row of delta or a column of xq with infinities or NaN gives infinities or NaN
  * there.  rows == 0: the sums are empty (cleared, or left where accumulated).  in == 0 or out == 0: no-op, OK.
  * ------------------------------------------------------------------------------------------- */
 size_t vgc_wgrad_checkpoint_workspace_bytes(int rows, int in, int out, vgc_type type);

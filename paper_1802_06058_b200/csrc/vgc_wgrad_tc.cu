@@ -12,7 +12,7 @@
 // leave each block the accumulators of its inputs.  In every block
 //   warp 0        one thread: TMA loads (codes, their scales, delta) into the raw ring
 //   warp 1        (of the first block) one thread: tcgen05.mma, operands in shared memory, both with the reduction outermost (MN-major)
-//   warps 4-11    two groups of four on alternate slices: codes -> xq, xq^2; delta -> its squares' parts (and its own, fp32)
+//   warps 4-11    groups of two or four, a slice each: codes -> xq, xq^2; delta -> its squares' parts (and its own, fp32)
 //   warps 12-19   four for g, four for S: every 256 rows they take the accumulator out of tensor memory and add it to running fp32
 //                 sums in registers (the tensor core truncates as it accumulates, about 1.3e-8 of the sum an instruction: 4e-7 over a run of
 //                 32), two accumulators in turn; at the end they write the tile, a lane an input: rows of 128 bytes
@@ -33,21 +33,25 @@ constexpr int kTileI = 256, kTile = 128, kHalf = 64;                // inputs, o
 constexpr int kSlice = 32, kChunk = 8;                              // rows; slices per run of an accumulator
 constexpr uint32_t kOperand = kSlice * kTile * 2, kErrors = kSlice * kHalf * 2;      // 8 KB, 4 KB: a bf16 operand of one slice
 constexpr uint32_t kCodes = kSlice * kTile, kScales = kSlice * 4;
-constexpr int kFirstTransform = 4, kGroups = 2, kFirstEpilogue = kFirstTransform + 4 * kGroups, kThreads = 32 * (kFirstEpilogue + 8);
+constexpr int kFirstTransform = 4, kTransformWarps = 8;
+constexpr int kFirstEpilogue = kFirstTransform + kTransformWarps, kThreads = 32 * (kFirstEpilogue + 8);
 constexpr int kRegsLaunch = 96, kRegsFew = 40, kRegsTransform = 56, kRegsEpilogue = 160;
-static_assert(128 * (kRegsFew + kGroups * kRegsTransform + 2 * kRegsEpilogue) <= kRegsLaunch * kThreads && kThreads * kRegsLaunch <= 65536,
+static_assert(128 * (kRegsFew + 2 * kRegsTransform + 2 * kRegsEpilogue) <= kRegsLaunch * kThreads && kThreads * kRegsLaunch <= 65536,
               "the shares come out of what the block was launched with");
 // kParts: bf16 parts of delta.  One: the raw tile is the operand.  Three (fp32): they stand behind xq and xq^2, then those of the square.
-// The ring's sizes are even: the slot's previous user is then the same group of transform warps.
 template <int kParts> struct Ring {
     static constexpr int kRaw = kParts == 1 ? 10 : 4, kOp = kParts == 1 ? 6 : 4;
+    // Transform warps take a slice in groups: many where the work on a slice is small beside its waits (bf16, 16384 x 4096 -> 16384: 6.3 ms with
+    // two groups, 6.1 with four), fewer where it is more (fp32, 128 x 784 -> 1024: 10.1 us with two, 11.3 with four).
+    static constexpr int kGroups = kParts == 1 ? 4 : 2, kGroupWarps = kTransformWarps / kGroups, kGroupThreads = 32 * kGroupWarps;
     static constexpr int kSquareParts = kParts == 1 ? 2 : 3;
     static constexpr uint32_t kDelta = kParts == 1 ? kErrors : 2 * kErrors;
     static constexpr uint32_t kRawBytes = kDelta + kCodes;          // [delta][codes]; the slots' scales lie behind both rings
     static constexpr uint32_t kOpBytes = 2 * kOperand + ((kParts == 1 ? 0 : 3) + kSquareParts) * kErrors;
     static constexpr uint32_t kOpBase = kRaw * kRawBytes;
     static constexpr uint32_t kScaleBase = kOpBase + kOp * kOpBytes, kSmem = kScaleBase + kRaw * kScales + 1024 /*align*/;
-    static_assert(kRaw % 2 == 0 && kOp % 2 == 0 && kRawBytes % 1024 == 0 && kSmem + 512 <= 232448, "");
+    // (see the transform's waits)
+    static_assert(kRaw >= kOp && kOp >= kGroups && kRawBytes % 1024 == 0 && kSmem + 512 <= 232448, "");
 };
 
 struct Params {
@@ -247,7 +251,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
             mbar_init(smem_u32(&raw_empty[i]), 1);
         }
         for (int i = 0; i < R::kOp; ++i) {
-            mbar_init(smem_u32(&op_full[i]), 8);             // of both blocks (the second's own stay unused)
+            mbar_init(smem_u32(&op_full[i]), 2 * R::kGroupWarps);             // of both blocks (the second's own stay unused)
             mbar_init(smem_u32(&op_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -359,22 +363,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
     } else if (warp < (uint32_t)kFirstEpilogue) {
         // ================= transform =================
         regs_dec<kRegsTransform>();
-        const int tt = (int)(threadIdx.x - 32 * kFirstTransform) & 127, group = (int)(warp - kFirstTransform) >> 2;
+        constexpr int kGroups = R::kGroups, kGroupThreads = R::kGroupThreads;
+        const int tt = (int)(threadIdx.x - 32 * kFirstTransform) % kGroupThreads, group = (int)(warp - kFirstTransform) / R::kGroupWarps;
         int total = 0;
         while (walk.next()) total += walk.s1 - walk.s0;
         for (int i = group; i < total; i += kGroups) {
             const int raw = i % R::kRaw, op = i % R::kOp;
+            // A parity tells two neighbouring phases apart.  Products retire in order: this group has seen those of slice i - kGroups - kOp
+            // retired, so those of i - 2 kOp are; with those of i - kOp retired, slice i - kRaw has been loaded.
             if (!mbar_wait(smem_u32(&op_empty[op]), ((uint32_t)(i / R::kOp) & 1u) ^ 1u, &abort_flag, 0)) break;
             if (!mbar_wait(smem_u32(&raw_full[raw]), (uint32_t)(i / R::kRaw) & 1u, &abort_flag, 0)) break;
             const uint8_t *const in = smem_gen + (uint32_t)raw * R::kRawBytes;
             uint8_t *const ops = smem_gen + R::kOpBase + (uint32_t)op * R::kOpBytes;
-            // codes: 32 rows of eight 16-byte pieces, two a thread.  Lanes of the right 64 columns take their halves the other way round:
+            // codes: 32 rows of eight 16-byte pieces.  Lanes of the right 64 columns take their halves the other way round:
             // eight lanes that store together then fill the banks.
             const uint32_t piece = tt & 7, side = piece >> 2;
             const uint8_t *const scales = smem_gen + R::kScaleBase + (uint32_t)raw * kScales + (piece >> 1);
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t k = (uint32_t)(tt >> 3) + 16 * u;
+#pragma unroll 2
+            for (int u = 0; u < kSlice * 8 / kGroupThreads; ++u) {
+                const uint32_t k = (uint32_t)(tt >> 3) + kGroupThreads / 8 * u;
                 const uint4 q = *reinterpret_cast<const uint4 *>(in + R::kDelta + k * kTile + 16 * piece);
                 const uint32_t bits = (uint32_t)scales[4 * k] << 23;
                 const uint64_t scale = (uint64_t)bits << 32 | bits;
@@ -396,8 +403,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
             if constexpr (kParts == 1) {                 // 256 pieces of eight errors, each to the same place
                 uint8_t *const squares = ops + 2 * kOperand;
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t at = 16 * (tt + 128 * u);
+                for (int u = 0; u < 256 / kGroupThreads; ++u) {
+                    const uint32_t at = 16 * (tt + kGroupThreads * u);
                     const uint4 d = *reinterpret_cast<const uint4 *>(in + at);
                     uint4 h, l;
                     h.x = square_hi(d.x); h.y = square_hi(d.y); h.z = square_hi(d.z); h.w = square_hi(d.w);
@@ -407,10 +414,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
                 }
             } else {                                     // raw: boxes of 32 columns, swizzled likewise
                 uint8_t *const parts = ops + 2 * kOperand;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t n = (uint32_t)tt + 128 * u, k = (n >> 2) & 31, col8 = (n & 3) + 4 * u;            // eight columns from 8 * col8 on
-                    const uint8_t *const row = in + u * 4096 + k * 128;
+#pragma unroll 1
+                for (int u = 0; u < 256 / kGroupThreads; ++u) {
+                    const uint32_t n = (uint32_t)(tt + kGroupThreads * u), k = (n >> 2) & 31, col8 = (n & 3) + 4 * (n >> 7);      // eight columns from 8 * col8 on
+                    const uint8_t *const row = in + (n >> 7) * 4096 + k * 128;
                     float v[8];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {

@@ -37,9 +37,12 @@ def check(x, delta, scale_g, scale_s, g, S):
         assert bool(((g.double() - scale_g * (d.t() @ q)).abs() <= 2e-6 * scale_g * (d.abs().t() @ q.abs())).all())
     if S is not None:
         want = scale_s * (d.square().t() @ q.square())
-        over = want > torch.finfo(torch.float32).max                     # fp32 has no such number
-        assert bool(torch.isinf(S[over]).all())
-        assert bool(((S.double() - want).abs() <= 1e-5 * want)[~over].all())
+        # The first part of a square is its nearest bf16, up to 2^-9 above it; so is the sum of first parts, before the later parts
+        # are added: within 2^-8 of fp32's largest number the sum may be infinite, and beyond it has to be.
+        most = torch.finfo(torch.float32).max
+        assert bool(torch.isinf(S[want > most * (1 + 2.0 ** -24)]).all())
+        near = (want > most * (1 - 2.0 ** -8)) & torch.isinf(S)
+        assert bool((((S.double() - want).abs() <= 1e-5 * want) | near).all())
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -76,6 +79,7 @@ def test_sizes_of_the_values(dtype, top):
     columns, the last row alone not zero."""
     rows, n_in, n_out = 600, 320, 200
     x, delta = activations(rows, n_in, torch.float32, 1), errors(rows, n_out, torch.float32, 2)
+    torch.manual_seed(top)
     x *= torch.logspace(-12, top, rows, device="cuda")[torch.randperm(rows, device="cuda")][:, None]
     delta *= torch.logspace(-9, top, rows, device="cuda")[torch.randperm(rows, device="cuda")][:, None]
     x[:, 64:96] = 0
