@@ -1,8 +1,7 @@
 // Layer norm over the rows of an activation matrix, its backward pass, and the gradient and squared-gradient sums of gain and bias.
 //
 // Forward: a row stays in the registers of its warps (8 features a lane, 16 beyond 8192) between the mean, the squared deviations
-// from it and the write: one read and one write of the matrix, no cancellation in the variance.  The next row is loaded before
-// the sums of this one.
+// from it and the write: one read and one write of the matrix, no cancellation in the variance.
 // Backward: dx = rstd (w - mean(w) - xh mean(w xh)), w = dy gamma.  The same lanes keep the column sums of their features (dy xh, dy
 // and their squares) in registers over all rows that their block takes, so x and dy are read once; each block leaves one row of
 // partial sums, which norm_combine adds in the blocks' order.
@@ -14,35 +13,90 @@
 // blocks of 256 columns need no sums across a row (x and dy are read twice).
 // Bound: HBM.
 #include <cfloat>
+#include <type_traits>
 
 #include "vgc_rowpass.cuh"
 
 namespace vgc {
 namespace {
 
-__device__ __forceinline__ float warp_sum(float v)
-{
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(~0u, v, d);
-    return v;
-}
-
-// Sums over the `warps` warps of a row, in every thread of them.  Two slots in turn: a warp writes a slot again only behind the
-// barrier of the sum after, when all have read it.
+// Sums of two values over the warps of a row.  post() shares the two out over the halves of a warp as it adds (5 shuffles for both) and
+// leaves the warp's in shared memory; behind settle(), a barrier of the row's warps, get() gives the row's in every thread.  A row's
+// work goes on between the two, so that neither the shuffles nor the barrier are waited for.  Two slots in turn: a warp posts into a
+// slot again only behind the barrier of the sums after, when all have got it.
 struct RowSum {
-    float2 *slots;                   // [2][32] of this group
+    float *slots;                    // [2][32 warps][2] of this group
     int warps, warp, lane, barrier, turn;
-    __device__ float2 operator()(float a, float b)
+    float mine;
+    __device__ __forceinline__ void post(float a, float b)
     {
-        a = warp_sum(a);
-        b = warp_sum(b);
-        if (warps == 1) return make_float2(a, b);
-        float2 *const s = slots + 32 * turn;
-        turn ^= 1;
-        if (lane == 0) s[warp] = make_float2(a, b);
-        asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
-        const float2 v = lane < warps ? s[lane] : make_float2(0.f, 0.f);
-        return make_float2(warp_sum(v.x), warp_sum(v.y));
+        const bool up = lane & 16;
+        float m = (up ? b : a) + __shfl_xor_sync(~0u, up ? a : b, 16);
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
+        mine = m;
+        if (warps > 1 && (lane & 15) == 0) slots[64 * turn + 2 * warp + (lane >> 4)] = m;
+    }
+    __device__ __forceinline__ void settle() const
+    {
+        if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
+    }
+    __device__ __forceinline__ float2 get()
+    {
+        float m = mine;
+        if (warps > 1) {
+            const float *const s = slots + 64 * turn + (lane >> 4);
+            turn ^= 1;
+            m = (lane & 15) < warps ? s[2 * (lane & 15)] : 0.f;
+            if (warps > 16) m += (lane & 15) + 16 < warps ? s[2 * (lane & 15) + 32] : 0.f;
+#pragma unroll
+            for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
+        }
+        const float other = __shfl_xor_sync(~0u, m, 16);
+        return lane & 16 ? make_float2(other, m) : make_float2(m, other);
+    }
+};
+
+__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
+constexpr int kBlock = 512;                                   // most threads of a block, and what an SM holds
+
+// How rows come into a block: kDepth of them under way in shared memory (rows that do not start on 16 bytes: one, in registers).
+// kArrays matrices are read.
+template <class T, bool kVec, int kParts, int kArrays>
+struct Rows {
+    static constexpr uint32_t kRow = 16 * kPieces16<T> * kParts * kArrays;                // bytes a thread
+    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kVec ? 1 : kFit > 8 ? 8 : kFit < 3 ? 3 : kFit;
+    static constexpr uint32_t smem(int threads) { return kVec ? kRow * kDepth * threads : 0; }
+    Raw<T> ahead[kVec ? 1 : kArrays][kVec ? 1 : kParts];
+    uint32_t base, threads;
+    int slot;                        // of the row that is taken next
+    __device__ __forceinline__ Rows(void *dynamic) : base(smem_at(dynamic) + 16 * threadIdx.x), threads(blockDim.x), slot(0) {}
+    __device__ __forceinline__ uint32_t place(int array, int part) const
+    {
+        return base + 16 * threads * kPieces16<T> * ((slot * kArrays + array) * kParts + part);
+    }
+    // asks for a row kDepth ahead of the one taken next; `row`: its first feature of this lane's warp, `left` features from there on
+    __device__ __forceinline__ void ask(int array, const T *row, int left, int lane)
+    {
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            if constexpr (kVec) ask_seg(place(array, k), threads, row + (left > k * kSeg ? k * kSeg : 0), left - k * kSeg, lane, true);
+            else load_seg<false>(row + k * kSeg, left - k * kSeg, lane, ahead[array][k]);
+        }
+    }
+    __device__ __forceinline__ void asked()                   // (or nothing was left to ask for)
+    {
+        if constexpr (kVec) copies_commit();
+        slot = slot + 1 == kDepth ? 0 : slot + 1;
+    }
+    __device__ __forceinline__ void take(int array, Raw<T> (&x)[kParts])
+    {
+        if constexpr (kVec) copies_wait<kDepth - 1>();
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            if constexpr (kVec) take_seg(place(array, k), threads, x[k]);
+            else x[k] = ahead[array][k];
+        }
     }
 };
 
@@ -53,88 +107,154 @@ struct Forward {
     const float *gamma, *beta;
     T *y;
     float *mean, *rstd;
-    int rows, features, warps, groups;      // warps of a row, rows a block takes at a time
+    int rows, features, warps, groups;      // warps of a row, groups of warps a block
     float eps;
+    bool vectors;                           // gain and bias both there and on 16 bytes
     Checkpoint c;
 };
 
-// kParts: segments of 256 features a warp takes
+// kParts: segments of 256 features a warp takes.  A group has three rows in hand: one whose mean is being added up, one whose squared
+// deviations are, one that is written; one barrier a row.
 template <class T, bool kVec, int kParts, bool kCheckpoint>
-__global__ void __launch_bounds__(1024, 1) norm_forward(const Forward<T> p)
+__global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
 {
-    __shared__ float2 slots[8][64];
+    using R = Rows<T, kVec, kParts, 1>;
+    extern __shared__ uint4 dynamic[];
+    __shared__ float slots[8][128];
     const int lane = threadIdx.x & 31, all = threadIdx.x >> 5, group = all / p.warps, warp = all - group * p.warps;
-    RowSum sum = {slots[group], p.warps, warp, lane, 1 + group, 0};
+    RowSum sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
     grid_release();
     grid_wait();
     const int C = p.features, first = warp * kParts * kSeg;
-    constexpr bool kKept = kParts == 1;      // gain and bias in registers
-    float gain[kKept ? 8 : 1], bias[kKept ? 8 : 1];
+    const bool full = first + kParts * kSeg <= C;
+    constexpr bool kKept = kParts <= 2;      // gain and bias in registers
+    F2 gain[kKept ? kParts : 1][4], bias[kKept ? kParts : 1][4];
+    auto vector = [&](const float *v, int at, int j, float otherwise) {
+        const int c0 = at + seg_col<T, kVec>(2 * j, lane), c1 = at + seg_col<T, kVec>(2 * j + 1, lane);
+        return f2(v && c0 < C ? ld_f(v + c0) : otherwise, v && c1 < C ? ld_f(v + c1) : otherwise);
+    };
     if constexpr (kKept) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = first + seg_col<T, kVec>(i, lane);
-            gain[i] = p.gamma && c < C ? ld_f(p.gamma + c) : 1.f;
-            bias[i] = p.beta && c < C ? ld_f(p.beta + c) : 0.f;
-        }
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                gain[k][j] = vector(p.gamma, first + k * kSeg, j, 1.f);
+                bias[k][j] = vector(p.beta, first + k * kSeg, j, 0.f);
+            }
     }
     if (kCheckpoint && blockIdx.x == gridDim.x - 1) clear_row_padding(p.c, p.rows, threadIdx.x, blockDim.x);
     const float per = 1.f / (float)C;
-    const int step = gridDim.x * p.groups;
-    Raw<T> next[kParts];
-    long long row = (long long)blockIdx.x * p.groups + group;
-    auto load = [&](long long r) {
-#pragma unroll
-        for (int k = 0; k < kParts; ++k)
-            if (r < p.rows) load_seg<kVec>(p.x + (size_t)r * C + first + k * kSeg, C - first - k * kSeg, lane, next[k]);
-    };
-    load(row);
-    for (; row < p.rows; row += step) {
-        Raw<T> cur[kParts];
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) cur[k] = next[k];
-        load(row + step);
-        float a = 0.f;
-#pragma unroll
-        for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a += value(cur[k], i);
-        const float mean = sum(a, 0.f).x * per;
-        float q = 0.f;
-#pragma unroll
-        for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float d = value(cur[k], i) - mean;
-                if (first + k * kSeg + seg_col<T, kVec>(i, lane) < C) q = fmaf(d, d, q);
-            }
-        const float rstd = 1.f / sqrtf(sum(q, 0.f).x * per + p.eps);
-        if (threadIdx.x % (32 * p.warps) == 0) {
-            p.mean[row] = mean;
-            p.rstd[row] = rstd;
+    const int step = (int)gridDim.x * p.groups, row0 = (int)blockIdx.x * p.groups + group;
+    const int count = row0 < p.rows ? (p.rows - 1 - row0) / step + 1 : 0;
+    const size_t stride = (size_t)step * C;
+    const T *from = p.x + (size_t)row0 * C + first;
+    T *to = p.y + (size_t)row0 * C + first;
+    R rows(dynamic);
+    int asked = 0;
+    auto ask = [&]() {
+        if (asked < count) {
+            rows.ask(0, from, C - first, lane);
+            from += stride;
         }
+        ++asked;
+        rows.asked();
+    };
+#pragma unroll
+    for (int d = 0; d < R::kDepth; ++d) ask();
+    Raw<T> x0[kParts], x1[kParts], x2[kParts];
+    float mean1 = 0.f, mean2 = 0.f;
+    for (int i = 0; i < count + 2; ++i) {
+        const float2 total = sum.get();                       // of the step before: row i - 1's sum, row i - 2's squares
+        float a = 0.f, q = 0.f;
+        if (i < count) {
+            rows.take(0, x0);
+            ask();                                            // (into the slot just read)
+            F2 v = 0;
+#pragma unroll
+            for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v = add2(v, pair_of(x0[k], j));
+            a = lo_of(v) + hi_of(v);
+        }
+        if (i >= 1 && i <= count) {
+            mean1 = total.x * per;
+            const F2 minus = f2(-mean1);
+            F2 v = 0;
+            if (full) {
+#pragma unroll
+                for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const F2 d = add2(pair_of(x1[k], j), minus);
+                        v = fma2(d, d, v);
+                    }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kParts; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const F2 d = add2(pair_of(x1[k], j), minus);
+                        const int c = first + k * kSeg;
+                        v = fma2(f2(c + seg_col<T, kVec>(2 * j, lane) < C ? lo_of(d) : 0.f, c + seg_col<T, kVec>(2 * j + 1, lane) < C ? hi_of(d) : 0.f), d, v);
+                    }
+            }
+            q = lo_of(v) + hi_of(v);
+        }
+        sum.post(a, q);
+        if (i >= 2) {
+            const int r = row0 + (i - 2) * step;
+            const float rstd = rsqrtf(total.y * per + p.eps);
+            if (warp == 0 && lane == 0) {
+                p.mean[r] = mean2;
+                p.rstd[r] = rstd;
+            }
+            const F2 minus = f2(-mean2), times = f2(rstd);
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) {
+                const int c = first + k * kSeg;
+                Raw<T> out;
+                F2 g[4], b[4];
+                if constexpr (kKept) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        g[j] = gain[kKept ? k : 0][j];
+                        b[j] = bias[kKept ? k : 0][j];
+                    }
+                } else if (kVec && full && p.vectors) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {             // four neighbouring features
+                        const int at = c + seg_col<T, kVec>(4 * h, lane);
+                        const uint4 u = ld_16(p.gamma + at), w = ld_16(p.beta + at);
+                        g[2 * h] = f2(__uint_as_float(u.x), __uint_as_float(u.y));
+                        g[2 * h + 1] = f2(__uint_as_float(u.z), __uint_as_float(u.w));
+                        b[2 * h] = f2(__uint_as_float(w.x), __uint_as_float(w.y));
+                        b[2 * h + 1] = f2(__uint_as_float(w.z), __uint_as_float(w.w));
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        g[j] = vector(p.gamma, c, j, 1.f);
+                        b[j] = vector(p.beta, c, j, 0.f);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    F2 v = fma2(mul2(add2(pair_of(x2[k], j), minus), times), g[j], b[j]);
+                    if (kCheckpoint && !full) v = f2(c + seg_col<T, kVec>(2 * j, lane) < C ? lo_of(v) : 0.f, c + seg_col<T, kVec>(2 * j + 1, lane) < C ? hi_of(v) : 0.f);
+                    set_pair(out, j, v);
+                }
+                store_seg<kVec>(to + k * kSeg, C - c, lane, out);
+                if (kCheckpoint && c < p.c.wide) store_blocks<T, kVec>(p.c, r, c, lane, out);
+            }
+            to += stride;
+        }
+        sum.settle();
 #pragma unroll
         for (int k = 0; k < kParts; ++k) {
-            const int at = first + k * kSeg;
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float g, b;
-                if constexpr (kKept) {
-                    g = gain[i];
-                    b = bias[i];
-                } else {
-                    const int c = at + seg_col<T, kVec>(i, lane);
-                    g = p.gamma && c < C ? ld_f(p.gamma + c) : 1.f;
-                    b = p.beta && c < C ? ld_f(p.beta + c) : 0.f;
-                }
-                v[i] = fmaf((value(cur[k], i) - mean) * rstd, g, b);
-                if (kCheckpoint && at + seg_col<T, kVec>(i, lane) >= C) v[i] = 0.f;
-            }
-            const Raw<T> out = to_raw(v, T());
-            store_seg<kVec>(p.y + (size_t)row * C + at, C - at, lane, out);
-            if (kCheckpoint && at < p.c.wide) store_blocks<T, kVec>(p.c, (int)row, at, lane, out);
+            x2[k] = x1[k];
+            x1[k] = x0[k];
         }
+        mean2 = mean1;
     }
 }
 
@@ -147,26 +267,29 @@ vgc_status forward_as(const void *x, const float *gamma, const float *beta, int 
     p.y = static_cast<T *>(y);
     p.gamma = gamma; p.beta = beta; p.mean = mean; p.rstd = rstd;
     p.rows = rows; p.features = features; p.eps = eps;
+    p.vectors = gamma && beta && aligned16(gamma) && aligned16(beta);
     p.c = {};
     if (checkpoint) p.c = checkpoint_at(checkpoint, rows, features);
-    const int parts = features > 32 * kSeg ? 2 : 1;
+    const int parts = features > 32 * kSeg ? 4 : features > 4 * kSeg ? 2 : 1;
     p.warps = (features + parts * kSeg - 1) / (parts * kSeg);
     // eight warps a block where rows are short, but no fewer blocks than SMs
     p.groups = p.warps <= 8 ? 8 / p.warps : 1;
     const int spread = (rows + kSmCount - 1) / kSmCount;
     if (p.groups > spread) p.groups = spread;
-    const int threads = 32 * p.warps * p.groups, resident = kSmCount * (1024 / threads);
+    const int threads = 32 * p.warps * p.groups, resident = kSmCount * (kBlock / threads);
     const int need = (int)(((long long)rows + p.groups - 1) / p.groups);
-    const bool vec = (size_t)features * sizeof(T) % 16 == 0;
-    auto pick = [&](auto part) {
+    auto start = [&](auto part, auto vector) -> vgc_status {
         constexpr int kParts = decltype(part)::value;
-        return checkpoint ? (vec ? norm_forward<T, true, kParts, true> : norm_forward<T, false, kParts, true>)
-                          : (vec ? norm_forward<T, true, kParts, false> : norm_forward<T, false, kParts, false>);
+        constexpr bool kVec = decltype(vector)::value;
+        using R = Rows<T, kVec, kParts, 1>;
+        const auto fn = checkpoint ? norm_forward<T, kVec, kParts, true> : norm_forward<T, kVec, kParts, false>;
+        if (kVec) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
+        VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)(need < resident ? need : resident)), dim3((unsigned)threads), R::smem(threads), st, true, p));
+        count_launch();
+        return VGC_OK;
     };
-    auto fn = parts == 2 ? pick(std::integral_constant<int, 2>()) : pick(std::integral_constant<int, 1>());
-    VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)(need < resident ? need : resident)), dim3((unsigned)threads), 0, st, true, p));
-    count_launch();
-    return VGC_OK;
+    auto with = [&](auto part) { return (size_t)features * sizeof(T) % 16 == 0 ? start(part, std::true_type()) : start(part, std::false_type()); };
+    return parts == 4 ? with(std::integral_constant<int, 4>()) : parts == 2 ? with(std::integral_constant<int, 2>()) : with(std::integral_constant<int, 1>());
 }
 
 // ---- backward -----------------------------------------------------------------------------------------------------------------
@@ -175,20 +298,20 @@ enum { kRows = 0, kSamples = 1, kPieces = 2 };
 struct Plan {
     bool wide;                       // the rows' two means come from norm_row_sums
     int mode, parts, warps, groups, blocks, pieces, length;      // kPieces: pieces of a sample, rows of a piece
-    int sums;                        // columns sums that a block leaves
+    int sums;                        // column sums that a block leaves
     size_t row_sums_bytes, bytes;
 };
 Plan plan_backward(int rows, int features, int per_example)
 {
     Plan p;
-    p.wide = features > 32 * kSeg;
+    const int samples = rows / per_example;
+    // (six sums of 16 features a lane, as whole samples take, are too many for its registers)
+    p.wide = features > 32 * kSeg || (features > 16 * kSeg && per_example > 1 && samples >= kSmCount);
     p.parts = !p.wide && features > 16 * kSeg ? 2 : 1;
     p.warps = p.wide ? 1 : (features + p.parts * kSeg - 1) / (p.parts * kSeg);
     p.groups = p.wide ? 8 : p.warps <= 8 ? 8 / p.warps : 1;
     const int slabs = p.wide ? (features + kSeg - 1) / kSeg : 1, threads = 32 * p.warps * p.groups;
-    // blocks that an SM holds, next to one another: by registers
-    const int resident = kSmCount * (threads <= 256 ? 2 : 1);
-    const int target = (resident + slabs - 1) / slabs, samples = rows / per_example;
+    const int target = (kSmCount * (kBlock / threads) + slabs - 1) / slabs;
     p.pieces = 1;
     p.length = per_example;
     if (per_example == 1) {
@@ -199,8 +322,8 @@ Plan plan_backward(int rows, int features, int per_example)
         p.mode = kSamples;
         p.blocks = target;
     } else {
-        p.mode = kPieces;
-        p.pieces = (target + samples - 1) / samples;
+        p.mode = kPieces;                                     // in one round of blocks, if there are not more samples than that
+        p.pieces = samples < target ? target / samples : 1;
         const int most = (per_example + p.groups - 1) / p.groups;
         if (p.pieces > most) p.pieces = most;
         p.length = (per_example + p.pieces - 1) / p.pieces;
@@ -224,120 +347,163 @@ struct Backward {
     int per_example, pieces, length;
 };
 
+// A group has two rows in hand: one whose means and column sums are being added up, and the one before it, which is written.
 template <class T, bool kVec, int kParts, int kMode, bool kWide>
-__global__ void __launch_bounds__(512, 1) norm_backward(const Backward<T> p)
+__global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
 {
-    __shared__ float2 slots[8][64];
+    using R = Rows<T, kVec, kParts, 2>;
+    extern __shared__ uint4 dynamic[];
+    __shared__ float slots[8][128];
     __shared__ float joined[kParts == 1 ? 8 * kSeg : 1];      // column sums of a block's groups: groups * warps <= 8
     const int lane = threadIdx.x & 31, all = threadIdx.x >> 5, group = all / p.warps, warp = all - group * p.warps;
-    RowSum sum = {slots[group], p.warps, warp, lane, 1 + group, 0};
+    RowSum sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
     grid_release();
     grid_wait();
     const int C = p.features, first = (kWide ? blockIdx.y * kSeg : 0) + warp * kParts * kSeg;
-    float gain[kParts][8];
-    float xh_dy[kParts][8] = {}, dy_sum[kParts][8] = {};                       // of all rows, or of the running sample
+    F2 gain[kParts][4];
+    F2 xh_dy[kParts][4] = {}, dy_sum[kParts][4] = {};                          // of all rows, or of the running sample
     constexpr int kKept = kMode == kSamples ? 2 : 0, kSquares = kMode == kPieces ? 0 : 2;
-    float kept[kKept ? 2 : 1][kParts][8] = {}, squares[kSquares ? 2 : 1][kParts][8] = {};
+    F2 kept[kKept ? 2 : 1][kParts][4] = {}, squares[kSquares ? 2 : 1][kParts][4] = {};
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = first + k * kSeg + seg_col<T, kVec>(i, lane);
-            gain[k][i] = c >= C ? 0.f : p.gamma ? ld_f(p.gamma + c) : 1.f;
+        for (int j = 0; j < 4; ++j) {
+            const int c0 = first + k * kSeg + seg_col<T, kVec>(2 * j, lane), c1 = first + k * kSeg + seg_col<T, kVec>(2 * j + 1, lane);
+            gain[k][j] = f2(c0 >= C ? 0.f : p.gamma ? ld_f(p.gamma + c0) : 1.f, c1 >= C ? 0.f : p.gamma ? ld_f(p.gamma + c1) : 1.f);
         }
 
-    // the rows of this group: from `row` on in steps, up to `end`; whole samples in steps of samples
-    long long row, end, step;
-    int left = 0;                                             // rows of the sample behind this one
+    // the rows of this group, `count` of them: `step` apart, or whole samples' rows one after another, samples `step` rows apart
+    int row, count, step, jump = 0;
     if constexpr (kMode == kPieces) {
         const int sample = blockIdx.x / p.pieces, piece = blockIdx.x - sample * p.pieces;
-        const long long start = (long long)sample * p.per_example;
-        row = start + (long long)piece * p.length + group;
-        end = min(start + p.per_example, start + (long long)(piece + 1) * p.length);
+        const int begin = piece * p.length + group, end = min(p.per_example, (piece + 1) * p.length);
+        row = sample * p.per_example + begin;
         step = p.groups;
+        count = begin < end ? (end - 1 - begin) / step + 1 : 0;
     } else {
-        row = ((long long)blockIdx.x * p.groups + group) * p.per_example;
-        step = (long long)gridDim.x * p.groups * p.per_example;
-        end = p.rows;
-        left = p.per_example - 1;
+        const int samples = p.rows / p.per_example, each = (int)gridDim.x * p.groups, mine = (int)blockIdx.x * p.groups + group;
+        row = mine < samples ? mine * p.per_example : 0;
+        count = mine < samples ? ((samples - 1 - mine) / each + 1) * p.per_example : 0;
+        step = kMode == kSamples ? 1 : each;
+        jump = kMode == kSamples ? (each - 1) * p.per_example : 0;              // over the other groups' samples
     }
-    auto after = [&](long long r) {                           // the row behind row r
-        if constexpr (kMode == kSamples) return left > 0 ? r + 1 : r + step - (p.per_example - 1);
-        else return r + step;
-    };
-    const float per = 1.f / (float)C;
-    Raw<T> next_x[kParts], next_d[kParts];
-    float next_mean = 0.f, next_rstd = 0.f;
-    float2 next_sums = make_float2(0.f, 0.f);
-    auto load = [&](long long r) {
-        if (r >= end) return;
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            load_seg<kVec>(p.x + (size_t)r * C + first + k * kSeg, C - first - k * kSeg, lane, next_x[k]);
-            load_seg<kVec>(p.dy + (size_t)r * C + first + k * kSeg, C - first - k * kSeg, lane, next_d[k]);
+    // what moves from row to row: an index, and how many rows of its sample are left behind it
+    struct Cursor {
+        uint32_t row;                                         // (steps past the last row: 2^31 rows and more)
+        int left;
+        __device__ __forceinline__ void next(int step, int jump, int per)
+        {
+            row += (uint32_t)step;
+            if constexpr (kMode == kSamples) {
+                if (left == 0) {
+                    row += (uint32_t)jump;
+                    left = per;
+                }
+                --left;
+            }
         }
+    };
+    const Cursor start = {(uint32_t)row, p.per_example - 1};
+    Cursor ahead = start, here = start, written = start;
+    const float per = 1.f / (float)C;
+    R rows(dynamic);
+    int asked = 0;
+    auto ask = [&]() {
+        if (asked < count) {
+            const size_t at = (size_t)ahead.row * C + first;
+            rows.ask(0, p.x + at, C - first, lane);
+            rows.ask(1, p.dy + at, C - first, lane);
+            ahead.next(step, jump, p.per_example);
+        }
+        ++asked;
+        rows.asked();
+    };
+#pragma unroll
+    for (int d = 0; d < R::kDepth; ++d) ask();
+    // a row's own numbers, one row ahead
+    float next_mean = 0.f, next_rstd = 0.f;
+    float2 next_sums = make_float2(0.f, 0.f), sums0 = next_sums, sums1 = next_sums;
+    auto ask_numbers = [&](uint32_t r) {
         next_mean = ld_f(p.mean + r);
         next_rstd = ld_f(p.rstd + r);
-        if (kWide) next_sums = make_float2(ld_f(&p.row_sums[r].x), ld_f(&p.row_sums[r].y));
+        if constexpr (kWide) next_sums = make_float2(ld_f(&p.row_sums[r].x), ld_f(&p.row_sums[r].y));
     };
-    load(row);
-    while (row < end) {
-        Raw<T> x[kParts], d[kParts];
+    if (count > 0) ask_numbers(start.row);
+    Raw<T> x0[kParts], d0[kParts], x1[kParts], d1[kParts];
+    float mean0 = 0.f, rstd0 = 0.f, mean1 = 0.f, rstd1 = 0.f;
+    for (int i = 0; i <= count; ++i) {
+        float2 total = make_float2(0.f, 0.f);
+        if constexpr (!kWide) total = sum.get();              // of the row before
+        float a_sum = 0.f, b_sum = 0.f;
+        if (i < count) {
+            rows.take(0, x0);
+            rows.take(1, d0);
+            ask();                                            // (into the slot just read)
+            mean0 = next_mean;
+            rstd0 = next_rstd;
+            sums0 = next_sums;
+            const bool last = kMode == kSamples && here.left == 0;
+            here.next(step, jump, p.per_example);
+            if (i + 1 < count) ask_numbers(here.row);
+            const F2 minus = f2(-mean0), times = f2(rstd0);
+            F2 a = 0, b = 0;
 #pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            x[k] = next_x[k];
-            d[k] = next_d[k];
-        }
-        const float mean = next_mean, rstd = next_rstd;
-        float2 means = next_sums;
-        const long long behind = after(row);
-        load(behind);
-        float a = 0.f, b = 0.f;
+            for (int k = 0; k < kParts; ++k)
 #pragma unroll
-        for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float xh = (value(x[k], i) - mean) * rstd, dy = value(d[k], i), t = dy * xh, w = dy * gain[k][i];
-                xh_dy[k][i] += t;
-                dy_sum[k][i] += dy;
-                if constexpr (kMode == kRows) {
-                    squares[0][k][i] = fmaf(t, t, squares[0][k][i]);
-                    squares[1][k][i] = fmaf(dy, dy, squares[1][k][i]);
+                for (int j = 0; j < 4; ++j) {
+                    const F2 dy = pair_of(d0[k], j), t = mul2(dy, mul2(add2(pair_of(x0[k], j), minus), times));
+                    xh_dy[k][j] = add2(xh_dy[k][j], t);
+                    dy_sum[k][j] = add2(dy_sum[k][j], dy);
+                    if constexpr (kMode == kRows) {
+                        squares[0][k][j] = fma2(t, t, squares[0][k][j]);
+                        squares[1][k][j] = fma2(dy, dy, squares[1][k][j]);
+                    }
+                    if constexpr (!kWide) {
+                        a = fma2(dy, gain[k][j], a);
+                        b = fma2(t, gain[k][j], b);
+                    }
                 }
-                a += w;
-                b = fmaf(w, xh, b);
-            }
-        if constexpr (!kWide) {
-            means = sum(a, b);
-            means.x *= per;
-            means.y *= per;
-        }
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float xh = (value(x[k], i) - mean) * rstd, w = value(d[k], i) * gain[k][i];
-                v[i] = rstd * (w - means.x - xh * means.y);
-            }
-            store_seg<kVec>(p.dx + (size_t)row * C + first + k * kSeg, C - first - k * kSeg, lane, to_raw(v, T()));
-        }
-        if constexpr (kMode == kSamples) {
-            if (left == 0) {
+            if (kMode == kSamples && last) {
 #pragma unroll
                 for (int k = 0; k < kParts; ++k)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        kept[0][k][i] += xh_dy[k][i];
-                        kept[1][k][i] += dy_sum[k][i];
-                        squares[0][k][i] = fmaf(xh_dy[k][i], xh_dy[k][i], squares[0][k][i]);
-                        squares[1][k][i] = fmaf(dy_sum[k][i], dy_sum[k][i], squares[1][k][i]);
-                        xh_dy[k][i] = dy_sum[k][i] = 0.f;
+                    for (int j = 0; j < 4; ++j) {
+                        kept[0][k][j] = add2(kept[0][k][j], xh_dy[k][j]);
+                        kept[1][k][j] = add2(kept[1][k][j], dy_sum[k][j]);
+                        squares[0][k][j] = fma2(xh_dy[k][j], xh_dy[k][j], squares[0][k][j]);
+                        squares[1][k][j] = fma2(dy_sum[k][j], dy_sum[k][j], squares[1][k][j]);
+                        xh_dy[k][j] = dy_sum[k][j] = 0;
                     }
             }
-            left = left == 0 ? p.per_example - 1 : left - 1;
+            a_sum = lo_of(a) + hi_of(a);
+            b_sum = lo_of(b) + hi_of(b);
         }
-        row = behind;
+        if constexpr (!kWide) sum.post(a_sum, b_sum);
+        if (i >= 1) {
+            const float2 means = kWide ? sums1 : make_float2(total.x * per, total.y * per);
+            const F2 minus = f2(-mean1), times = f2(rstd1), less = f2(-means.x), by = f2(-means.y);
+            T *const to = p.dx + (size_t)written.row * C + first;
+#pragma unroll
+            for (int k = 0; k < kParts; ++k) {
+                Raw<T> out;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const F2 xh = mul2(add2(pair_of(x1[k], j), minus), times);
+                    set_pair(out, j, mul2(fma2(xh, by, fma2(pair_of(d1[k], j), gain[k][j], less)), times));
+                }
+                store_seg<kVec>(to + k * kSeg, C - first - k * kSeg, lane, out);
+            }
+            written.next(step, jump, p.per_example);
+        }
+        if constexpr (!kWide) sum.settle();
+#pragma unroll
+        for (int k = 0; k < kParts; ++k) {
+            x1[k] = x0[k];
+            d1[k] = d0[k];
+        }
+        mean1 = mean0;
+        rstd1 = rstd0;
+        sums1 = sums0;
     }
 
     // the groups' sums in the groups' order, then the block's row of partial sums
@@ -348,8 +514,11 @@ __global__ void __launch_bounds__(512, 1) norm_backward(const Backward<T> p)
 #pragma unroll
         for (int k = 0; k < kParts; ++k)
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[k][i] = q >= 2 ? squares[kSquares ? q - 2 : 0][k][i] : kMode == kSamples ? kept[kKept ? q : 0][k][i] : q == 0 ? xh_dy[k][i] : dy_sum[k][i];
+            for (int j = 0; j < 4; ++j) {
+                const F2 s = q >= 2 ? squares[kSquares ? q - 2 : 0][k][j] : kMode == kSamples ? kept[kKept ? q : 0][k][j] : q == 0 ? xh_dy[k][j] : dy_sum[k][j];
+                v[k][2 * j] = lo_of(s);
+                v[k][2 * j + 1] = hi_of(s);
+            }
         if constexpr (kParts == 1) {
             if (p.groups > 1) {
                 __syncthreads();
@@ -376,9 +545,9 @@ __global__ void __launch_bounds__(512, 1) norm_backward(const Backward<T> p)
 template <class T, bool kVec>
 __global__ void __launch_bounds__(512) norm_row_sums(const Backward<T> p, float2 *out)
 {
-    __shared__ float2 slots[64];
+    __shared__ float slots[128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, C = p.features;
-    RowSum sum = {slots, warps, warp, lane, 1, 0};
+    RowSum sum = {slots, warps, warp, lane, 1, 0, 0.f};
     grid_release();
     grid_wait();
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
@@ -396,12 +565,14 @@ __global__ void __launch_bounds__(512) norm_row_sums(const Backward<T> p, float2
                 b = fmaf(w, (value(x, i) - mean) * rstd, b);
             }
         }
-        const float2 s = sum(a, b);
+        sum.post(a, b);
+        sum.settle();
+        const float2 s = sum.get();
         if (threadIdx.x == 0) out[row] = make_float2(s.x / (float)C, s.y / (float)C);
     }
 }
 
-// The blocks' partial sums of 32 features, each of eight warps an eighth of them, added in order.
+// The blocks' partial sums of 32 features, each of 16 warps a sixteenth of them, added in order.
 // samples == 0: partial [n][4][C].  Otherwise [samples][pieces][2][C]: a sample's pieces are added, then squared.
 struct Combine {
     const float *partial;
@@ -410,9 +581,10 @@ struct Combine {
     int accumulate_g, accumulate_s;
     float *out[4];                   // g_gamma, g_beta, s_gamma, s_beta
 };
-__global__ void __launch_bounds__(256) norm_combine(const Combine p)
+constexpr int kCombineWarps = 16;
+__global__ void __launch_bounds__(32 * kCombineWarps) norm_combine(const Combine p)
 {
-    __shared__ float part[4][8][32];
+    __shared__ float part[4][kCombineWarps][32];
     grid_release();
     grid_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
@@ -420,13 +592,13 @@ __global__ void __launch_bounds__(256) norm_combine(const Combine p)
     float v[4] = {};
     if (c < p.features) {
         if (p.samples == 0) {
-            const int each = (p.n + 7) / 8, last = min(p.n, (warp + 1) * each);
+            const int each = (p.n + kCombineWarps - 1) / kCombineWarps, last = min(p.n, (warp + 1) * each);
 #pragma unroll 4
             for (int b = warp * each; b < last; ++b)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) v[q] += ld_f(p.partial + ((size_t)b * 4 + q) * C + c);
         } else {
-            const int each = (p.samples + 7) / 8, last = min(p.samples, (warp + 1) * each);
+            const int each = (p.samples + kCombineWarps - 1) / kCombineWarps, last = min(p.samples, (warp + 1) * each);
             for (int s = warp * each; s < last; ++s) {
                 float a = 0.f, b = 0.f;
 #pragma unroll 4
@@ -449,7 +621,7 @@ __global__ void __launch_bounds__(256) norm_combine(const Combine p)
     if (warp >= 4 || c >= p.features || !to) return;
     float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += part[warp][w][lane];
+    for (int w = 0; w < kCombineWarps; ++w) s += part[warp][w][lane];
     s *= warp < 2 ? p.scale_g : p.scale_s;
     to[c] = (warp < 2 ? p.accumulate_g : p.accumulate_s) ? ld_f(to + c) + s : s;
 }
@@ -475,18 +647,29 @@ vgc_status backward_as(const void *x, const void *dy, const float *gamma, const 
                                   dim3(512), 0, st, true, p, row_sums));
         count_launch();
     }
-    auto pick = [&](auto mode) {
-        constexpr int kMode = decltype(mode)::value;
-        if (plan.wide) return vec ? norm_backward<T, true, 1, kMode, true> : norm_backward<T, false, 1, kMode, true>;
-        if (plan.parts == 2) return vec ? norm_backward<T, true, 2, kMode, false> : norm_backward<T, false, 2, kMode, false>;
-        return vec ? norm_backward<T, true, 1, kMode, false> : norm_backward<T, false, 1, kMode, false>;
+    auto start = [&](auto mode, auto vector, auto part, auto wide) -> vgc_status {
+        constexpr bool kVec = decltype(vector)::value;
+        constexpr int kParts = decltype(part)::value;
+        using R = Rows<T, kVec, kParts, 2>;
+        const int threads = 32 * plan.warps * plan.groups;
+        const auto fn = norm_backward<T, kVec, kParts, decltype(mode)::value, decltype(wide)::value>;
+        if (kVec) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
+        VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks, plan.wide ? (unsigned)((features + kSeg - 1) / kSeg) : 1u), dim3((unsigned)threads),
+                                  R::smem(threads), st, true, p));
+        count_launch();
+        return VGC_OK;
     };
-    auto fn = plan.mode == kRows ? pick(std::integral_constant<int, kRows>())
-              : plan.mode == kSamples ? pick(std::integral_constant<int, kSamples>()) : pick(std::integral_constant<int, kPieces>());
-    VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks, plan.wide ? (unsigned)((features + kSeg - 1) / kSeg) : 1u),
-                              dim3((unsigned)(32 * plan.warps * plan.groups)), 0, st, true, p));
-    count_launch();
-    return VGC_OK;
+    const std::integral_constant<int, 1> one;
+    const std::integral_constant<int, 2> two;
+    auto shaped = [&](auto mode, auto vector) {
+        if (plan.wide) return start(mode, vector, one, std::true_type());
+        if constexpr (decltype(mode)::value != kSamples)
+            if (plan.parts == 2) return start(mode, vector, two, std::false_type());
+        return start(mode, vector, one, std::false_type());
+    };
+    auto with = [&](auto mode) { return vec ? shaped(mode, std::true_type()) : shaped(mode, std::false_type()); };
+    return plan.mode == kRows ? with(std::integral_constant<int, kRows>())
+           : plan.mode == kSamples ? with(std::integral_constant<int, kSamples>()) : with(std::integral_constant<int, kPieces>());
 }
 
 bool type_ok(vgc_type type) { return type == VGC_FP32 || type == VGC_BF16; }
@@ -554,7 +737,7 @@ extern "C" vgc_status vgc_layernorm_backward(const void *x, const void *dy, vgc_
     c.samples = plan.mode == kPieces ? rows / rows_per_example : 0;
     c.pieces = plan.pieces;
     c.features = features; c.scale_g = scale_g; c.scale_s = scale_s;
-    VGC_CUDA_OK(launch_kernel(norm_combine, dim3((unsigned)((features + 31) / 32)), dim3(256), 0, st, true, c));
+    VGC_CUDA_OK(launch_kernel(norm_combine, dim3((unsigned)((features + 31) / 32)), dim3(32 * kCombineWarps), 0, st, true, c));
     count_launch();
     return VGC_OK;
 }

@@ -134,6 +134,86 @@ __device__ __forceinline__ void store_seg(__nv_bfloat16 *seg, int left, int lane
     }
 }
 
+// ---- pairs of fp32 in one 64-bit register: half the instructions (each component rounded as by the plain operation) ---------------
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float a, float b)
+{
+    F2 v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+    return v;
+}
+__device__ __forceinline__ F2 f2(float a) { return f2(a, a); }
+__device__ __forceinline__ float lo_of(F2 v) { return __uint_as_float((uint32_t)v); }
+__device__ __forceinline__ float hi_of(F2 v) { return __uint_as_float((uint32_t)(v >> 32)); }
+__device__ __forceinline__ F2 add2(F2 a, F2 b)
+{
+    F2 v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b)
+{
+    F2 v;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c)
+{
+    F2 v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+// features 2j and 2j + 1 of a lane's 8
+__device__ __forceinline__ F2 pair_of(const Raw<float> &r, int j) { return f2(r.v[2 * j], r.v[2 * j + 1]); }
+__device__ __forceinline__ F2 pair_of(const Raw<__nv_bfloat16> &r, int j)
+{
+    return f2(__uint_as_float(r.v[j] << 16), __uint_as_float(r.v[j] & 0xFFFF0000u));
+}
+__device__ __forceinline__ void set_pair(Raw<float> &r, int j, F2 v) { r.v[2 * j] = lo_of(v); r.v[2 * j + 1] = hi_of(v); }
+__device__ __forceinline__ void set_pair(Raw<__nv_bfloat16> &r, int j, F2 v) { r.v[j] = bf16_pair(lo_of(v), hi_of(v)); }
+
+// ---- a lane's pieces of coming rows, on their way through shared memory: every thread reads what it asked for itself, so that no
+// barrier is needed.  Slots of 16-byte pieces, `threads` of them side by side.
+__device__ __forceinline__ void copy_16(uint32_t smem, const void *from, bool wanted)
+{
+    const uint32_t bytes = wanted ? 16u : 0u;                 // (0: the piece becomes zeros, nothing is read)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+__device__ __forceinline__ uint4 ld_shared_16(uint32_t smem)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem) : "memory");
+    return v;
+}
+template <class T> constexpr int kPieces16 = (int)sizeof(T) / 2;    // 16-byte pieces of 8 features
+// `seg`, `left` as for load_seg; rows == false: zeros
+template <class T>
+__device__ __forceinline__ void ask_seg(uint32_t slot, uint32_t threads, const T *seg, int left, int lane, bool row)
+{
+#pragma unroll
+    for (int j = 0; j < kPieces16<T>; ++j) {
+        const int c = sizeof(T) == 2 ? 8 * lane : 128 * j + 4 * lane;
+        const bool wanted = row && c < left;
+        copy_16(slot + 16 * threads * j, wanted ? seg + c : seg, wanted);
+    }
+}
+__device__ __forceinline__ void take_seg(uint32_t slot, uint32_t threads, Raw<float> &r)
+{
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint4 v = ld_shared_16(slot + 16 * threads * j);
+        r.v[4 * j] = __uint_as_float(v.x); r.v[4 * j + 1] = __uint_as_float(v.y);
+        r.v[4 * j + 2] = __uint_as_float(v.z); r.v[4 * j + 3] = __uint_as_float(v.w);
+    }
+}
+__device__ __forceinline__ void take_seg(uint32_t slot, uint32_t, Raw<__nv_bfloat16> &r)
+{
+    const uint4 v = ld_shared_16(slot);
+    r.v[0] = v.x; r.v[1] = v.y; r.v[2] = v.z; r.v[3] = v.w;
+}
+
 // ---- 8-bit checkpoints: codes [rows][wide] e4m3, scale exponents [wide / 128][tall][4] ---------------------------------------
 struct Checkpoint {
     uint8_t *codes;
