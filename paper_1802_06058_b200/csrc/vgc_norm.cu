@@ -20,81 +20,117 @@
 namespace vgc {
 namespace {
 
-// Sums of two values over the warps of a row.  post() shares the two out over the halves of a warp as it adds (5 shuffles for both) and
-// leaves the warp's in shared memory; behind settle(), a barrier of the row's warps, get() gives the row's in every thread.  A row's
-// work goes on between the two, so that neither the shuffles nor the barrier are waited for.  Two slots in turn: a warp posts into a
-// slot again only behind the barrier of the sums after, when all have got it.
+// Sums of N values, 2 or 4, over the warps of a row.  post() shares the values out over a warp's lanes as it adds (5 or 6 shuffles for all
+// of them) and leaves the warp's sums in shared memory; behind settle(), a barrier of the row's warps, get() gives the row's in every
+// thread.  Other rows' work between the two hides the
+// shuffles and the barrier.  Two slots in turn: a
+// warp posts into a slot again only behind the barrier of the sums after, when all have got it.
+constexpr int kBlock = 512;                                   // most threads of a block, and what an SM holds
+
+template <int N>
 struct RowSum {
-    float *slots;                    // [2][32 warps][2] of this group
+    static constexpr int kLanes = 32 / N;                     // lanes of a value, neighbours
+    float *slots;                    // [2][32 warps][N] of this group
     int warps, warp, lane, barrier, turn;
     float mine;
-    __device__ __forceinline__ void post(float a, float b)
+    __device__ __forceinline__ void post(const float (&v)[N])
     {
-        const bool up = lane & 16;
-        float m = (up ? b : a) + __shfl_xor_sync(~0u, up ? a : b, 16);
+        const bool up = lane & 16, right = lane & 8;
+        float m;
+        if constexpr (N == 2) {
+            m = (up ? v[1] : v[0]) + __shfl_xor_sync(~0u, up ? v[0] : v[1], 16);
+        } else {
+            const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(~0u, up ? v[0] : v[2], 16);
+            const float b = (up ? v[3] : v[1]) + __shfl_xor_sync(~0u, up ? v[1] : v[3], 16);
+            m = (right ? b : a) + __shfl_xor_sync(~0u, right ? a : b, 8);
+        }
 #pragma unroll
-        for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
+        for (int d = kLanes / 2; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
         mine = m;
-        if (warps > 1 && (lane & 15) == 0) slots[64 * turn + 2 * warp + (lane >> 4)] = m;
+        if (warps > 1 && lane % kLanes == 0) slots[32 * N * turn + N * warp + lane / kLanes] = m;
     }
     __device__ __forceinline__ void settle() const
     {
         if (warps > 1) asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(32 * warps) : "memory");
     }
-    __device__ __forceinline__ float2 get()
+    __device__ __forceinline__ void get(float (&v)[N])
     {
         float m = mine;
         if (warps > 1) {
-            const float *const s = slots + 64 * turn + (lane >> 4);
+            const float *const s = slots + 32 * N * turn + lane / kLanes;
             turn ^= 1;
-            m = (lane & 15) < warps ? s[2 * (lane & 15)] : 0.f;
-            if (warps > 16) m += (lane & 15) + 16 < warps ? s[2 * (lane & 15) + 32] : 0.f;
+            m = 0.f;
 #pragma unroll
-            for (int d = 8; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
+            for (int w = 0; w < kBlock / 32; w += kLanes)
+                if (w < warps) m += w + lane % kLanes < warps ? s[N * (w + lane % kLanes)] : 0.f;
+#pragma unroll
+            for (int d = kLanes / 2; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
         }
-        const float other = __shfl_xor_sync(~0u, m, 16);
-        return lane & 16 ? make_float2(other, m) : make_float2(m, other);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __shfl_sync(~0u, m, kLanes * i);
     }
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-constexpr int kBlock = 512;                                   // most threads of a block, and what an SM holds
 
 // How rows come into a block: kDepth of them under way in shared memory (rows that do not start on 16 bytes: one, in registers).
 // kArrays matrices are read.
 template <class T, bool kVec, int kParts, int kArrays>
 struct Rows {
-    static constexpr uint32_t kRow = 16 * kPieces16<T> * kParts * kArrays;                // bytes a thread
+    static constexpr int kPieces = kPieces16<T>;
+    static constexpr uint32_t kRow = 16 * kPieces * kParts * kArrays;                     // bytes a thread
     static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kVec ? 1 : kFit > 8 ? 8 : kFit < 3 ? 3 : kFit;
     static constexpr uint32_t smem(int threads) { return kVec ? kRow * kDepth * threads : 0; }
     Raw<T> ahead[kVec ? 1 : kArrays][kVec ? 1 : kParts];
-    uint32_t base, threads;
-    int slot;                        // of the row that is taken next
-    __device__ __forceinline__ Rows(void *dynamic) : base(smem_at(dynamic) + 16 * threadIdx.x), threads(blockDim.x), slot(0) {}
-    __device__ __forceinline__ uint32_t place(int array, int part) const
+    uint32_t begin, end, at, pitch;  // the ring of this thread's pieces, the row taken next
+    uint32_t offset[kParts][kPieces], bytes[kParts][kPieces];       // this lane's pieces of a warp's features; 0 past the row's end
+    int left, lane;
+    // left: features of a row from the warp's first one on
+    __device__ __forceinline__ Rows(void *dynamic, int left_, int lane_) : left(left_), lane(lane_)
     {
-        return base + 16 * threads * kPieces16<T> * ((slot * kArrays + array) * kParts + part);
+        pitch = 16 * blockDim.x;
+        at = begin = smem_at(dynamic) + 16 * threadIdx.x;
+        end = begin + pitch * (kRow / 16) * kDepth;
+#pragma unroll
+        for (int k = 0; k < kParts; ++k)
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int c = k * kSeg + (sizeof(T) == 2 ? 8 * lane : 128 * j + 4 * lane);
+                bytes[k][j] = c < left ? 16 : 0;
+                offset[k][j] = c < left ? c * (int)sizeof(T) : 0;
+            }
     }
-    // asks for a row kDepth ahead of the one taken next; `row`: its first feature of this lane's warp, `left` features from there on
-    __device__ __forceinline__ void ask(int array, const T *row, int left, int lane)
+    // asks for a row kDepth ahead of the one taken next; `row`: its first feature of this warp
+    __device__ __forceinline__ void ask(int array, const T *row)
     {
 #pragma unroll
         for (int k = 0; k < kParts; ++k) {
-            if constexpr (kVec) ask_seg(place(array, k), threads, row + (left > k * kSeg ? k * kSeg : 0), left - k * kSeg, lane, true);
-            else load_seg<false>(row + k * kSeg, left - k * kSeg, lane, ahead[array][k]);
+            if constexpr (kVec) {
+#pragma unroll
+                for (int j = 0; j < kPieces; ++j)
+                    copy_16(at + pitch * ((array * kParts + k) * kPieces + j), reinterpret_cast<const char *>(row) + offset[k][j], bytes[k][j]);
+            } else {
+                load_seg<false>(row + k * kSeg, left - k * kSeg, lane, ahead[array][k]);
+            }
         }
     }
     __device__ __forceinline__ void asked()                   // (or nothing was left to ask for)
     {
-        if constexpr (kVec) copies_commit();
-        slot = slot + 1 == kDepth ? 0 : slot + 1;
+        if constexpr (kVec) {
+            copies_commit();
+            at += pitch * (kRow / 16);
+            at = at == end ? begin : at;
+        }
+    }
+    __device__ __forceinline__ void arrived() const
+    {
+        if constexpr (kVec) copies_wait<kDepth - 1>();
     }
     __device__ __forceinline__ void take(int array, Raw<T> (&x)[kParts])
     {
-        if constexpr (kVec) copies_wait<kDepth - 1>();
 #pragma unroll
         for (int k = 0; k < kParts; ++k) {
-            if constexpr (kVec) take_seg(place(array, k), threads, x[k]);
+            if constexpr (kVec) take_seg(at + pitch * (array * kParts + k) * kPieces, pitch, x[k]);
             else x[k] = ahead[array][k];
         }
     }
@@ -122,7 +158,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
     extern __shared__ uint4 dynamic[];
     __shared__ float slots[8][128];
     const int lane = threadIdx.x & 31, all = threadIdx.x >> 5, group = all / p.warps, warp = all - group * p.warps;
-    RowSum sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
+    RowSum<2> sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
     grid_release();
     grid_wait();
     const int C = p.features, first = warp * kParts * kSeg;
@@ -149,11 +185,11 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
     const size_t stride = (size_t)step * C;
     const T *from = p.x + (size_t)row0 * C + first;
     T *to = p.y + (size_t)row0 * C + first;
-    R rows(dynamic);
+    R rows(dynamic, C - first, lane);
     int asked = 0;
     auto ask = [&]() {
         if (asked < count) {
-            rows.ask(0, from, C - first, lane);
+            rows.ask(0, from);
             from += stride;
         }
         ++asked;
@@ -164,9 +200,11 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
     Raw<T> x0[kParts], x1[kParts], x2[kParts];
     float mean1 = 0.f, mean2 = 0.f;
     for (int i = 0; i < count + 2; ++i) {
-        const float2 total = sum.get();                       // of the step before: row i - 1's sum, row i - 2's squares
+        float total[2];                                       // of the step before: row i - 1's sum, row i - 2's squares
+        sum.get(total);
         float a = 0.f, q = 0.f;
         if (i < count) {
+            rows.arrived();
             rows.take(0, x0);
             ask();                                            // (into the slot just read)
             F2 v = 0;
@@ -177,7 +215,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
             a = lo_of(v) + hi_of(v);
         }
         if (i >= 1 && i <= count) {
-            mean1 = total.x * per;
+            mean1 = total[0] * per;
             const F2 minus = f2(-mean1);
             F2 v = 0;
             if (full) {
@@ -200,10 +238,10 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
             }
             q = lo_of(v) + hi_of(v);
         }
-        sum.post(a, q);
+        sum.post({a, q});
         if (i >= 2) {
             const int r = row0 + (i - 2) * step;
-            const float rstd = rsqrtf(total.y * per + p.eps);
+            const float rstd = rsqrtf(total[1] * per + p.eps);
             if (warp == 0 && lane == 0) {
                 p.mean[r] = mean2;
                 p.rstd[r] = rstd;
@@ -347,16 +385,20 @@ struct Backward {
     int per_example, pieces, length;
 };
 
-// A group has two rows in hand: one whose means and column sums are being added up, and the one before it, which is written.
+// kAt rows at a time, so that the wait for their sums over the row is shared.  (fp32 rows of single elements and 16 features a lane have
+// no registers for two.)  A lane keeps the rows' dy and xh between the sums and the write, or, where it has 16 features, the rows
+// themselves.
 template <class T, bool kVec, int kParts, int kMode, bool kWide>
 __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
 {
     using R = Rows<T, kVec, kParts, 2>;
+    constexpr int kAt = kVec && kParts == 1 ? 2 : 1;
+    constexpr bool kAgain = kParts > 1;      // xh worked out again for the write
     extern __shared__ uint4 dynamic[];
-    __shared__ float slots[8][128];
+    __shared__ float slots[8][128 * kAt];
     __shared__ float joined[kParts == 1 ? 8 * kSeg : 1];      // column sums of a block's groups: groups * warps <= 8
     const int lane = threadIdx.x & 31, all = threadIdx.x >> 5, group = all / p.warps, warp = all - group * p.warps;
-    RowSum sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
+    RowSum<2 * kAt> sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
     grid_release();
     grid_wait();
     const int C = p.features, first = (kWide ? blockIdx.y * kSeg : 0) + warp * kParts * kSeg;
@@ -404,106 +446,139 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
         }
     };
     const Cursor start = {(uint32_t)row, p.per_example - 1};
-    Cursor ahead = start, here = start, written = start;
+    Cursor ahead = start, here = start;
     const float per = 1.f / (float)C;
-    R rows(dynamic);
+    R rows(dynamic, C - first, lane);
     int asked = 0;
+    // the rows' own numbers, a step ahead
+    float next_mean[kAt] = {}, next_rstd[kAt] = {};
+    float2 next_sums[kAt] = {};
     auto ask = [&]() {
         if (asked < count) {
             const size_t at = (size_t)ahead.row * C + first;
-            rows.ask(0, p.x + at, C - first, lane);
-            rows.ask(1, p.dy + at, C - first, lane);
+            rows.ask(0, p.x + at);
+            rows.ask(1, p.dy + at);
             ahead.next(step, jump, p.per_example);
         }
         ++asked;
         rows.asked();
     };
+    Cursor numbers = start;
+    int numbered = 0;
+    auto ask_numbers = [&]() {
+#pragma unroll
+        for (int at = 0; at < kAt; ++at)
+            if (numbered + at < count) {
+                next_mean[at] = ld_f(p.mean + numbers.row);
+                next_rstd[at] = ld_f(p.rstd + numbers.row);
+                if constexpr (kWide) next_sums[at] = make_float2(ld_f(&p.row_sums[numbers.row].x), ld_f(&p.row_sums[numbers.row].y));
+                numbers.next(step, jump, p.per_example);
+            }
+        numbered += kAt;
+    };
 #pragma unroll
     for (int d = 0; d < R::kDepth; ++d) ask();
-    // a row's own numbers, one row ahead
-    float next_mean = 0.f, next_rstd = 0.f;
-    float2 next_sums = make_float2(0.f, 0.f), sums0 = next_sums, sums1 = next_sums;
-    auto ask_numbers = [&](uint32_t r) {
-        next_mean = ld_f(p.mean + r);
-        next_rstd = ld_f(p.rstd + r);
-        if constexpr (kWide) next_sums = make_float2(ld_f(&p.row_sums[r].x), ld_f(&p.row_sums[r].y));
-    };
-    if (count > 0) ask_numbers(start.row);
-    Raw<T> x0[kParts], d0[kParts], x1[kParts], d1[kParts];
-    float mean0 = 0.f, rstd0 = 0.f, mean1 = 0.f, rstd1 = 0.f;
-    for (int i = 0; i <= count; ++i) {
-        float2 total = make_float2(0.f, 0.f);
-        if constexpr (!kWide) total = sum.get();              // of the row before
-        float a_sum = 0.f, b_sum = 0.f;
-        if (i < count) {
-            rows.take(0, x0);
-            rows.take(1, d0);
-            ask();                                            // (into the slot just read)
-            mean0 = next_mean;
-            rstd0 = next_rstd;
-            sums0 = next_sums;
-            const bool last = kMode == kSamples && here.left == 0;
-            here.next(step, jump, p.per_example);
-            if (i + 1 < count) ask_numbers(here.row);
-            const F2 minus = f2(-mean0), times = f2(rstd0);
+    ask_numbers();
+    for (int i = 0; i < count; i += kAt) {
+        Raw<T> x[kAt][kParts], d[kAt][kParts];
+        F2 xh[kAgain ? 1 : kAt][4], dy[kAgain ? 1 : kAt][4];
+        F2 minus[kAt], times[kAt];
+        float v[2 * kAt] = {};
+#pragma unroll
+        for (int at = 0; at < kAt; ++at) {
+            if (kAt > 1 && i + at >= count) {                 // a row that is not there: zeros add nothing
+                x[at][0] = d[at][0] = {};
+                minus[at] = times[at] = 0;
+            } else {
+                rows.arrived();
+                rows.take(0, x[at]);
+                rows.take(1, d[at]);
+                ask();                                        // (into the slot just read)
+                minus[at] = f2(-next_mean[at]);
+                times[at] = f2(next_rstd[at]);
+                if constexpr (kWide) {
+                    v[2 * at] = next_sums[at].x;
+                    v[2 * at + 1] = next_sums[at].y;
+                }
+            }
+        }
+        ask_numbers();
+        Cursor this_row = here;
+#pragma unroll
+        for (int at = 0; at < kAt; ++at) {
             F2 a = 0, b = 0;
 #pragma unroll
             for (int k = 0; k < kParts; ++k)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const F2 dy = pair_of(d0[k], j), t = mul2(dy, mul2(add2(pair_of(x0[k], j), minus), times));
+                    const F2 e = pair_of(d[at][k], j), h = mul2(add2(pair_of(x[at][k], j), minus[at]), times[at]), t = mul2(e, h);
+                    if constexpr (!kAgain) {
+                        xh[at][j] = h;
+                        dy[at][j] = e;
+                    }
                     xh_dy[k][j] = add2(xh_dy[k][j], t);
-                    dy_sum[k][j] = add2(dy_sum[k][j], dy);
+                    dy_sum[k][j] = add2(dy_sum[k][j], e);
                     if constexpr (kMode == kRows) {
                         squares[0][k][j] = fma2(t, t, squares[0][k][j]);
-                        squares[1][k][j] = fma2(dy, dy, squares[1][k][j]);
+                        squares[1][k][j] = fma2(e, e, squares[1][k][j]);
                     }
                     if constexpr (!kWide) {
-                        a = fma2(dy, gain[k][j], a);
+                        a = fma2(e, gain[k][j], a);
                         b = fma2(t, gain[k][j], b);
                     }
                 }
-            if (kMode == kSamples && last) {
+            if constexpr (kMode == kSamples) {
+                const bool last = this_row.left == 0 && i + at < count;
+                this_row.next(step, jump, p.per_example);
+                if (last) {
 #pragma unroll
-                for (int k = 0; k < kParts; ++k)
+                    for (int k = 0; k < kParts; ++k)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        kept[0][k][j] = add2(kept[0][k][j], xh_dy[k][j]);
-                        kept[1][k][j] = add2(kept[1][k][j], dy_sum[k][j]);
-                        squares[0][k][j] = fma2(xh_dy[k][j], xh_dy[k][j], squares[0][k][j]);
-                        squares[1][k][j] = fma2(dy_sum[k][j], dy_sum[k][j], squares[1][k][j]);
-                        xh_dy[k][j] = dy_sum[k][j] = 0;
-                    }
+                        for (int j = 0; j < 4; ++j) {
+                            kept[0][k][j] = add2(kept[0][k][j], xh_dy[k][j]);
+                            kept[1][k][j] = add2(kept[1][k][j], dy_sum[k][j]);
+                            squares[0][k][j] = fma2(xh_dy[k][j], xh_dy[k][j], squares[0][k][j]);
+                            squares[1][k][j] = fma2(dy_sum[k][j], dy_sum[k][j], squares[1][k][j]);
+                            xh_dy[k][j] = dy_sum[k][j] = 0;
+                        }
+                }
             }
-            a_sum = lo_of(a) + hi_of(a);
-            b_sum = lo_of(b) + hi_of(b);
+            if constexpr (!kWide) {
+                v[2 * at] = lo_of(a) + hi_of(a);
+                v[2 * at + 1] = lo_of(b) + hi_of(b);
+            }
         }
-        if constexpr (!kWide) sum.post(a_sum, b_sum);
-        if (i >= 1) {
-            const float2 means = kWide ? sums1 : make_float2(total.x * per, total.y * per);
-            const F2 minus = f2(-mean1), times = f2(rstd1), less = f2(-means.x), by = f2(-means.y);
-            T *const to = p.dx + (size_t)written.row * C + first;
+        if constexpr (!kWide) {
+            sum.post(v);
+            sum.settle();
+            sum.get(v);
+#pragma unroll
+            for (int n = 0; n < 2 * kAt; ++n) v[n] *= per;
+        }
+#pragma unroll
+        for (int at = 0; at < kAt; ++at) {
+            if (kAt > 1 && i + at >= count) break;
+            const F2 less = f2(-v[2 * at]), by = f2(-v[2 * at + 1]);
+            T *const to = p.dx + (size_t)here.row * C + first;
 #pragma unroll
             for (int k = 0; k < kParts; ++k) {
                 Raw<T> out;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const F2 xh = mul2(add2(pair_of(x1[k], j), minus), times);
-                    set_pair(out, j, mul2(fma2(xh, by, fma2(pair_of(d1[k], j), gain[k][j], less)), times));
+                    F2 h, e;
+                    if constexpr (kAgain) {
+                        h = mul2(add2(pair_of(x[at][k], j), minus[at]), times[at]);
+                        e = pair_of(d[at][k], j);
+                    } else {
+                        h = xh[at][j];
+                        e = dy[at][j];
+                    }
+                    set_pair(out, j, mul2(fma2(h, by, fma2(e, gain[k][j], less)), times[at]));
                 }
                 store_seg<kVec>(to + k * kSeg, C - first - k * kSeg, lane, out);
             }
-            written.next(step, jump, p.per_example);
+            here.next(step, jump, p.per_example);
         }
-        if constexpr (!kWide) sum.settle();
-#pragma unroll
-        for (int k = 0; k < kParts; ++k) {
-            x1[k] = x0[k];
-            d1[k] = d0[k];
-        }
-        mean1 = mean0;
-        rstd1 = rstd0;
-        sums1 = sums0;
     }
 
     // the groups' sums in the groups' order, then the block's row of partial sums
@@ -547,7 +622,7 @@ __global__ void __launch_bounds__(512) norm_row_sums(const Backward<T> p, float2
 {
     __shared__ float slots[128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, C = p.features;
-    RowSum sum = {slots, warps, warp, lane, 1, 0, 0.f};
+    RowSum<2> sum = {slots, warps, warp, lane, 1, 0, 0.f};
     grid_release();
     grid_wait();
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
@@ -565,10 +640,11 @@ __global__ void __launch_bounds__(512) norm_row_sums(const Backward<T> p, float2
                 b = fmaf(w, (value(x, i) - mean) * rstd, b);
             }
         }
-        sum.post(a, b);
+        sum.post({a, b});
         sum.settle();
-        const float2 s = sum.get();
-        if (threadIdx.x == 0) out[row] = make_float2(s.x / (float)C, s.y / (float)C);
+        float s[2];
+        sum.get(s);
+        if (threadIdx.x == 0) out[row] = make_float2(s[0] / (float)C, s[1] / (float)C);
     }
 }
 

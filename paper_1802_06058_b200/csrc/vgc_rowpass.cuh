@@ -174,9 +174,8 @@ __device__ __forceinline__ void set_pair(Raw<__nv_bfloat16> &r, int j, F2 v) { r
 
 // ---- a lane's pieces of coming rows, on their way through shared memory: every thread reads what it asked for itself, so that no
 // barrier is needed.  Slots of 16-byte pieces, `threads` of them side by side.
-__device__ __forceinline__ void copy_16(uint32_t smem, const void *from, bool wanted)
+__device__ __forceinline__ void copy_16(uint32_t smem, const void *from, uint32_t bytes)      // bytes 0: the piece becomes zeros, nothing is read
 {
-    const uint32_t bytes = wanted ? 16u : 0u;                 // (0: the piece becomes zeros, nothing is read)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(from), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -188,22 +187,12 @@ __device__ __forceinline__ uint4 ld_shared_16(uint32_t smem)
     return v;
 }
 template <class T> constexpr int kPieces16 = (int)sizeof(T) / 2;    // 16-byte pieces of 8 features
-// `seg`, `left` as for load_seg; rows == false: zeros
-template <class T>
-__device__ __forceinline__ void ask_seg(uint32_t slot, uint32_t threads, const T *seg, int left, int lane, bool row)
-{
-#pragma unroll
-    for (int j = 0; j < kPieces16<T>; ++j) {
-        const int c = sizeof(T) == 2 ? 8 * lane : 128 * j + 4 * lane;
-        const bool wanted = row && c < left;
-        copy_16(slot + 16 * threads * j, wanted ? seg + c : seg, wanted);
-    }
-}
-__device__ __forceinline__ void take_seg(uint32_t slot, uint32_t threads, Raw<float> &r)
+// `pitch`: bytes from one 16-byte piece of a thread to its next
+__device__ __forceinline__ void take_seg(uint32_t slot, uint32_t pitch, Raw<float> &r)
 {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-        const uint4 v = ld_shared_16(slot + 16 * threads * j);
+        const uint4 v = ld_shared_16(slot + pitch * j);
         r.v[4 * j] = __uint_as_float(v.x); r.v[4 * j + 1] = __uint_as_float(v.y);
         r.v[4 * j + 2] = __uint_as_float(v.z); r.v[4 * j + 3] = __uint_as_float(v.w);
     }
