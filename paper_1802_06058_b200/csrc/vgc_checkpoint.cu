@@ -10,32 +10,47 @@ namespace {
 
 constexpr int kThreads = 256, kFlight = 4;
 
-// segments are numbered along the rows: neighbouring warps read neighbouring memory
+// The segments that a warp takes, numbered along the rows: neighbouring warps work on neighbouring memory.
+struct Walk {
+    uint32_t row, seg, rows_on, segs_on, segs;
+    __device__ __forceinline__ Walk(uint32_t segs_) : segs(segs_)
+    {
+        const uint32_t warp = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5), warps = gridDim.x * (kThreads / 32);
+        row = warp / segs;
+        seg = warp - row * segs;
+        rows_on = warps / segs;
+        segs_on = warps - rows_on * segs;
+    }
+    __device__ __forceinline__ void next()
+    {
+        row += rows_on;
+        seg += segs_on;
+        if (seg >= segs) {
+            seg -= segs;
+            ++row;
+        }
+    }
+};
+
 template <class T, bool kVec>
 __global__ void __launch_bounds__(kThreads) checkpoint_store(const T *x, int rows, int features, uint32_t segs, Checkpoint c)
 {
     grid_release();
     grid_wait();
     const int lane = threadIdx.x & 31;
-    const uint64_t total = (uint64_t)rows * segs, warps = (uint64_t)gridDim.x * (kThreads / 32);
-    const uint64_t warp = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     if (blockIdx.x == gridDim.x - 1) clear_row_padding(c, rows, threadIdx.x, kThreads);
-    for (uint64_t s = warp; s < total; s += kFlight * warps) {
+    Walk ahead(segs), here = ahead;
+    while (here.row < (uint32_t)rows) {
         Raw<T> r[kFlight];
-        int row[kFlight], first[kFlight];
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const uint64_t at = s + k * warps;
-            if (at >= total) break;
-            row[k] = (int)(at / segs);
-            first[k] = (int)(at - (uint64_t)row[k] * segs) * kSeg;
-            load_seg<kVec>(x + (size_t)row[k] * features + first[k], features - first[k], lane, r[k]);
+        for (int k = 0; k < kFlight; ++k, ahead.next()) {
+            if (ahead.row >= (uint32_t)rows) continue;
+            const int first = (int)ahead.seg * kSeg;
+            load_seg<kVec>(x + (size_t)ahead.row * features + first, features - first, lane, r[k]);
         }
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            if (s + k * warps >= total) break;
-            store_blocks<T, kVec>(c, row[k], first[k], lane, r[k]);
-        }
+        for (int k = 0; k < kFlight; ++k, here.next())
+            if (here.row < (uint32_t)rows) store_blocks<T, kVec>(c, (int)here.row, (int)here.seg * kSeg, lane, r[k]);
     }
 }
 
@@ -46,31 +61,26 @@ __global__ void __launch_bounds__(kThreads) checkpoint_load(T *x, int rows, int 
     grid_release();
     grid_wait();
     const int lane = threadIdx.x & 31;
-    const uint64_t total = (uint64_t)rows * segs, warps = (uint64_t)gridDim.x * (kThreads / 32);
-    const uint64_t warp = (uint64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    for (uint64_t s = warp; s < total; s += kFlight * warps) {
+    Walk ahead(segs), here = ahead;
+    while (here.row < (uint32_t)rows) {
         uint32_t q[kFlight][2], w[kFlight][2];
-        int row[kFlight], first[kFlight];
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            const uint64_t at = s + k * warps;
-            if (at >= total) break;
-            row[k] = (int)(at / segs);
-            first[k] = (int)(at - (uint64_t)row[k] * segs) * kSeg;
-            const int left = c.wide - first[k], unit = first[k] >> 7;
-            const uint8_t *const codes = c.codes + (size_t)row[k] * c.wide + first[k];
+        for (int k = 0; k < kFlight; ++k, ahead.next()) {
+            if (ahead.row >= (uint32_t)rows) continue;
+            const int first = (int)ahead.seg * kSeg, left = c.wide - first, unit = first >> 7;
+            const uint8_t *const codes = c.codes + (size_t)ahead.row * c.wide + first;
             q[k][0] = q[k][1] = 0;
             if constexpr (kVec && sizeof(T) == 2) {
                 if (8 * lane < left) {
                     const uint2 v = *reinterpret_cast<const uint2 *>(codes + 8 * lane);
                     q[k][0] = v.x; q[k][1] = v.y;
-                    w[k][0] = *scale_word(c, row[k], unit + (lane >> 4));
+                    w[k][0] = *scale_word(c, (int)ahead.row, unit + (lane >> 4));
                 }
             } else {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     if (128 * j >= left) continue;
-                    w[k][j] = *scale_word(c, row[k], unit + j);
+                    w[k][j] = *scale_word(c, (int)ahead.row, unit + j);
                     if constexpr (kVec) {
                         q[k][j] = *reinterpret_cast<const uint32_t *>(codes + 128 * j + 4 * lane);
                     } else {
@@ -81,23 +91,21 @@ __global__ void __launch_bounds__(kThreads) checkpoint_load(T *x, int rows, int 
             }
         }
 #pragma unroll
-        for (int k = 0; k < kFlight; ++k) {
-            if (s + k * warps >= total) break;
-            float v[8];
+        for (int k = 0; k < kFlight; ++k, here.next()) {
+            if (here.row >= (uint32_t)rows) continue;
+            const int first = (int)here.seg * kSeg;
+            Raw<T> out;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                e4m3_values(q[k][j], v[4 * j], v[4 * j + 1]);
-                e4m3_values(q[k][j] >> 16, v[4 * j + 2], v[4 * j + 3]);
+            for (int j = 0; j < 4; ++j) {
+                float a, b;
+                e4m3_values(q[k][j >> 1] >> (16 * (j & 1)), a, b);
+                F2 scale;
+                if constexpr (!kVec) scale = f2(scale_of(w[k][j >> 1] >> (16 * (j & 1)) & 255u), scale_of(w[k][j >> 1] >> (16 * (j & 1) + 8) & 255u));
+                else if constexpr (sizeof(T) == 2) scale = f2(scale_of(w[k][0] >> (8 * ((lane >> 2) & 3)) & 255u));
+                else scale = f2(scale_of(w[k][j >> 1] >> (8 * (lane >> 3)) & 255u));
+                set_pair(out, j, mul2(f2(a, b), scale));
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                uint32_t e;
-                if constexpr (!kVec) e = w[k][i >> 2] >> (8 * (i & 3));
-                else if constexpr (sizeof(T) == 2) e = w[k][0] >> (8 * ((lane >> 2) & 3));
-                else e = w[k][i >> 2] >> (8 * (lane >> 3));
-                v[i] *= scale_of(e & 255u);
-            }
-            store_seg<kVec>(x + (size_t)row[k] * features + first[k], features - first[k], lane, to_raw(v, T()));
+            store_seg<kVec>(x + (size_t)here.row * features + first, features - first, lane, out);
         }
     }
 }

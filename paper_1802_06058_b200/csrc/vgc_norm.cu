@@ -79,8 +79,8 @@ template <class T, bool kVec, int kParts, int kArrays>
 struct Rows {
     static constexpr int kPieces = kPieces16<T>;
     static constexpr uint32_t kRow = 16 * kPieces * kParts * kArrays;                     // bytes a thread
-    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kVec ? 1 : kFit > 8 ? 8 : kFit < 3 ? 3 : kFit;
-    static constexpr uint32_t smem(int threads) { return kVec ? kRow * kDepth * threads : 0; }
+    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kVec ? 1 : kFit > 8 ? 8 : kFit < 3 && kArrays == 1 ? 3 : kFit;
+    __host__ __device__ static constexpr uint32_t smem(int threads) { return kVec ? kRow * kDepth * threads : 0; }
     Raw<T> ahead[kVec ? 1 : kArrays][kVec ? 1 : kParts];
     uint32_t begin, end, at, pitch;  // the ring of this thread's pieces, the row taken next
     uint32_t offset[kParts][kPieces], bytes[kParts][kPieces];       // this lane's pieces of a warp's features; 0 past the row's end
@@ -308,7 +308,8 @@ vgc_status forward_as(const void *x, const float *gamma, const float *beta, int 
     p.vectors = gamma && beta && aligned16(gamma) && aligned16(beta);
     p.c = {};
     if (checkpoint) p.c = checkpoint_at(checkpoint, rows, features);
-    const int parts = features > 32 * kSeg ? 4 : features > 4 * kSeg ? 2 : 1;
+    // (16384 x 4096 with the checkpoint: bf16 88 us with 16 features a lane and 102 with 8; fp32, short of registers, 150 and 127)
+    const int parts = features > 32 * kSeg ? 4 : features > (sizeof(T) == 2 ? 4 : 16) * kSeg ? 2 : 1;
     p.warps = (features + parts * kSeg - 1) / (parts * kSeg);
     // eight warps a block where rows are short, but no fewer blocks than SMs
     p.groups = p.warps <= 8 ? 8 / p.warps : 1;
@@ -393,6 +394,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
 {
     using R = Rows<T, kVec, kParts, 2>;
     constexpr int kAt = kVec && kParts == 1 ? 2 : 1;
+    constexpr bool kShared = kParts > 1 && kMode == kRows;    // the sums of squares lie in shared memory, every thread's own
     constexpr bool kAgain = kParts > 1;      // xh worked out again for the write
     extern __shared__ uint4 dynamic[];
     __shared__ float slots[8][128 * kAt];
@@ -406,6 +408,11 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
     F2 xh_dy[kParts][4] = {}, dy_sum[kParts][4] = {};                          // of all rows, or of the running sample
     constexpr int kKept = kMode == kSamples ? 2 : 0, kSquares = kMode == kPieces ? 0 : 2;
     F2 kept[kKept ? 2 : 1][kParts][4] = {}, squares[kSquares ? 2 : 1][kParts][4] = {};
+    const uint32_t own = smem_at(dynamic) + R::smem((int)blockDim.x) + 16 * threadIdx.x, own_pitch = 16 * blockDim.x;
+    if constexpr (kShared) {
+#pragma unroll
+        for (int n = 0; n < 4 * kParts; ++n) st_shared_16(own + own_pitch * n, make_uint4(0, 0, 0, 0));
+    }
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
@@ -487,7 +494,8 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
 #pragma unroll
         for (int at = 0; at < kAt; ++at) {
             if (kAt > 1 && i + at >= count) {                 // a row that is not there: zeros add nothing
-                x[at][0] = d[at][0] = {};
+#pragma unroll
+                for (int k = 0; k < kParts; ++k) x[at][k] = d[at][k] = {};
                 minus[at] = times[at] = 0;
             } else {
                 rows.arrived();
@@ -518,7 +526,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
                     }
                     xh_dy[k][j] = add2(xh_dy[k][j], t);
                     dy_sum[k][j] = add2(dy_sum[k][j], e);
-                    if constexpr (kMode == kRows) {
+                    if constexpr (kMode == kRows && !kShared) {
                         squares[0][k][j] = fma2(t, t, squares[0][k][j]);
                         squares[1][k][j] = fma2(e, e, squares[1][k][j]);
                     }
@@ -548,8 +556,27 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
                 v[2 * at + 1] = lo_of(b) + hi_of(b);
             }
         }
+        if constexpr (!kWide) sum.post(v);
+        if constexpr (kShared) {                              // (while the row's other warps come to the barrier)
+#pragma unroll
+            for (int n = 0; n < 4 * kParts; ++n) {
+                const int q = n / (2 * kParts), k = n / 2 % kParts, j = 2 * (n % 2);
+                const uint4 u = ld_shared_16(own + own_pitch * n);
+                F2 s0 = f2(__uint_as_float(u.x), __uint_as_float(u.y)), s1 = f2(__uint_as_float(u.z), __uint_as_float(u.w));
+#pragma unroll
+                for (int at = 0; at < kAt; ++at) {
+                    F2 t0 = pair_of(d[at][k], j), t1 = pair_of(d[at][k], j + 1);
+                    if (q == 0) {
+                        t0 = mul2(t0, mul2(add2(pair_of(x[at][k], j), minus[at]), times[at]));
+                        t1 = mul2(t1, mul2(add2(pair_of(x[at][k], j + 1), minus[at]), times[at]));
+                    }
+                    s0 = fma2(t0, t0, s0);
+                    s1 = fma2(t1, t1, s1);
+                }
+                st_shared_16(own + own_pitch * n, make_uint4((uint32_t)s0, (uint32_t)(s0 >> 32), (uint32_t)s1, (uint32_t)(s1 >> 32)));
+            }
+        }
         if constexpr (!kWide) {
-            sum.post(v);
             sum.settle();
             sum.get(v);
 #pragma unroll
@@ -578,6 +605,15 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
                 store_seg<kVec>(to + k * kSeg, C - first - k * kSeg, lane, out);
             }
             here.next(step, jump, p.per_example);
+        }
+    }
+
+    if constexpr (kShared) {
+#pragma unroll
+        for (int n = 0; n < 4 * kParts; ++n) {
+            const uint4 u = ld_shared_16(own + own_pitch * n);
+            squares[n / (2 * kParts)][n / 2 % kParts][2 * (n % 2)] = f2(__uint_as_float(u.x), __uint_as_float(u.y));
+            squares[n / (2 * kParts)][n / 2 % kParts][2 * (n % 2) + 1] = f2(__uint_as_float(u.z), __uint_as_float(u.w));
         }
     }
 
@@ -729,9 +765,11 @@ vgc_status backward_as(const void *x, const void *dy, const float *gamma, const 
         using R = Rows<T, kVec, kParts, 2>;
         const int threads = 32 * plan.warps * plan.groups;
         const auto fn = norm_backward<T, kVec, kParts, decltype(mode)::value, decltype(wide)::value>;
-        if (kVec) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
+        constexpr int kOwn = kParts > 1 && decltype(mode)::value == kRows ? 64 * kParts : 0;      // bytes a thread: its sums of squares
+        static_assert(R::smem(kBlock) + kOwn * kBlock + 16384 <= 232448, "");
+        if (kVec || kOwn) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock) + kOwn * kBlock));
         VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks, plan.wide ? (unsigned)((features + kSeg - 1) / kSeg) : 1u), dim3((unsigned)threads),
-                                  R::smem(threads), st, true, p));
+                                  R::smem(threads) + kOwn * threads, st, true, p));
         count_launch();
         return VGC_OK;
     };
