@@ -15,12 +15,6 @@ struct WgradArgs {
         v = __fmul_rn(scale, v);
         *to = accumulate ? __fadd_rn(ld_f(to), v) : v;
     }
-    __device__ __forceinline__ void write(int o, int i, float vg, float vs) const
-    {
-        const size_t at = (size_t)o * in + i;
-        if (g) write_one(g + at, vg, scale_g, accumulate_g);
-        if (S) write_one(S + at, vs, scale_s, accumulate_s);
-    }
 };
 
 size_t wgrad_tc_workspace_bytes(int rows, int in, int out, vgc_type type);

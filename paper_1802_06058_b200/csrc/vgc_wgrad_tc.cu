@@ -13,9 +13,8 @@
 //   warp 0        one thread: TMA loads (codes, their scales, delta) into the raw ring
 //   warp 1        (of the first block) one thread: tcgen05.mma, operands in shared memory, both with the reduction outermost (MN-major)
 //   warps 4-11    groups of two or four, a slice each: codes -> xq, xq^2; delta -> its squares' parts (and its own, fp32)
-//   warps 12-19   four for g, four for S: every 256 rows they take the accumulator out of tensor memory and add it to running fp32
-//                 sums in registers (the tensor core truncates as it accumulates, about 1.3e-8 of the sum an instruction: 4e-7 over a run of
-//                 32), two accumulators in turn; at the end they write the tile, a lane an input: rows of 128 bytes
+//   warps 12-19   four for g, four for S: every 128 or 256 rows they take the accumulator out of tensor memory and add it to running
+//                 fp32 sums in registers (the tensor core truncates as it accumulates), two accumulators in turn; at the end they write the tile, a lane an input: rows of 128 bytes
 // The work is the sequence of all tiles' slices.  Where whole tiles fill the SMs evenly, blocks take whole tiles; otherwise
 // every pair takes an equal stretch of the sequence, leaves the tiles it shares with its neighbours as partial sums, and
 // wgrad_combine adds those in the pairs' order.
@@ -30,7 +29,7 @@ namespace wgrad {
 using namespace tc;
 
 constexpr int kTileI = 256, kTile = 128, kHalf = 64;                // inputs, outputs of a pair; 128 and 64 a block
-constexpr int kSlice = 32, kChunk = 8;                              // rows; slices per run of an accumulator
+constexpr int kSlice = 32;                                          // rows
 constexpr uint32_t kOperand = kSlice * kTile * 2, kErrors = kSlice * kHalf * 2;      // 8 KB, 4 KB: a bf16 operand of one slice
 constexpr uint32_t kCodes = kSlice * kTile, kScales = kSlice * 4;
 constexpr int kFirstTransform = 4, kTransformWarps = 8;
@@ -60,7 +59,7 @@ struct Params {
     uint32_t *status;
     float *partial;                  // [2 * pairs][2][128 o][256 i]
     long long total;                 // slices of all tiles
-    int slices, tiles_i, tiles_o, wide, tall;
+    int slices, chunk, tiles_i, tiles_o, wide, tall;                // chunk: slices per run of an accumulator
     bool whole;                      // pairs take whole tiles, as many apart as there are pairs
 };
 constexpr size_t kPartial = (size_t)kTileI * kTile;                 // floats of one result
@@ -317,13 +316,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
             int it = 0, c = 0;
             bool ok = true;
             while (ok && walk.next()) {
-                for (int s0 = walk.s0; ok && s0 < walk.s1; s0 += kChunk, ++c) {
+                for (int s0 = walk.s0; ok && s0 < walk.s1; s0 += prm.chunk, ++c) {
                     const int b = c & 1;
                     ok = wait_pair(smem_u32(&acc_empty[b]), ((uint32_t)(c >> 1) & 1u) ^ 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     const uint32_t d_g = tmem_base + (uint32_t)b * 2 * kTile, d_s = d_g + kTile;
-                    const int s1 = min(walk.s1, s0 + kChunk);
+                    const int s1 = min(walk.s1, s0 + prm.chunk);
                     for (int s = s0; s < s1; ++s, ++it) {
                         const int raw = it % R::kRaw, op = it % R::kOp;
                         ok = wait_pair(smem_u32(&op_full[op]), (uint32_t)(it / R::kOp) & 1u, &abort_flag);
@@ -456,7 +455,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
             float sum[kTile];                            // (from zeros: set by the first run instead, they went through local memory)
 #pragma unroll
             for (int j = 0; j < kTile; ++j) sum[j] = 0.f;
-            for (int s0 = walk.s0; s0 < walk.s1; s0 += kChunk, ++c) {
+            for (int s0 = walk.s0; s0 < walk.s1; s0 += prm.chunk, ++c) {
                 const int b = c & 1;
                 ok = mbar_wait(smem_u32(&acc_full[b]), (uint32_t)(c >> 1) & 1u, &abort_flag, 32);
                 if (!ok) break;
@@ -625,6 +624,10 @@ vgc_status launch(const WgradArgs &args, const T *delta, const Checkpoint &c, vo
     p.scales = c.scales;
     p.status = static_cast<uint32_t *>(ws);
     p.partial = reinterpret_cast<float *>(space + 256);
+    // What an accumulator's truncation takes off S over a run, error of 256 rows with runs of 256 and of 128: 1.5e-6 and 0.7e-6 (bf16),
+    // 1.9e-6 and 0.9e-6 (fp32).  Over many runs rounding evens that out (4096 rows, bf16: 0.9e-6), and there a longer run saves 7 % of
+    // the time; with fp32's six products it saves 1 %.
+    p.chunk = kParts == 1 && plan.slices > 64 ? 8 : 4;
     p.slices = plan.slices; p.tiles_i = plan.tiles_i; p.tiles_o = plan.tiles_o; p.wide = c.wide; p.tall = c.tall; p.whole = plan.whole;
     p.total = (long long)plan.tiles_i * plan.tiles_o * plan.slices;
     const auto fn = wgrad_tiles<kParts>;
