@@ -506,7 +506,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
 }
 
 // The tiles that pairs share: blockIdx.x + 1 is the pair whose first slice lies inside the tile, the first such pair of the tile.
-// 256 threads take 16 outputs: four neighbouring inputs and four of the outputs each.
+// 256 threads take 16 outputs of g or of S: four neighbouring inputs and four of the outputs each.
 constexpr int kCombineRows = 16;
 __global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int pairs)
 {
@@ -528,29 +528,28 @@ __global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int pairs
     int i0, o0;
     tile_at(prm, found[0], i0, o0);
     const int i = (int)(threadIdx.x & 63) * 4, o = (int)(blockIdx.y * kCombineRows + (threadIdx.x >> 6) * 4);
+    float *const out = blockIdx.z == 0 ? prm.out.g : prm.out.S;
+    const float scale = blockIdx.z == 0 ? prm.out.scale_g : prm.out.scale_s;
+    const int accumulate = blockIdx.z == 0 ? prm.out.accumulate_g : prm.out.accumulate_s;
+    if (!out) return;
+    float sum[4][4];
+#pragma unroll 2
+    for (int k = 0; k < n; ++k) {                             // the first pair's last stretch, the others' first
+        const float *const from = prm.partial + ((size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * 2 + blockIdx.z) * kPartial + o * kTileI + i;
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        float *const out = which == 0 ? prm.out.g : prm.out.S;
-        if (!out) continue;
-        float sum[4][4];
-        for (int k = 0; k < n; ++k) {                         // the first pair's last stretch, the others' first
-            const float *const from = prm.partial + ((size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * 2 + which) * kPartial + o * kTileI + i;
+        for (int r = 0; r < 4; ++r) {
+            const uint4 v = ld_16(from + r * kTileI);
+            const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const uint4 v = ld_16(from + r * kTileI);
-                const float f[4] = {__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w)};
-#pragma unroll
-                for (int c = 0; c < 4; ++c) sum[r][c] = k == 0 ? f[c] : __fadd_rn(sum[r][c], f[c]);
-            }
+            for (int c = 0; c < 4; ++c) sum[r][c] = k == 0 ? f[c] : __fadd_rn(sum[r][c], f[c]);
         }
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (i0 + i + c < prm.out.in && o0 + o + r < prm.out.out)
-                    prm.out.write_one(out + (size_t)(o0 + o + r) * prm.out.in + i0 + i + c, sum[r][c], which == 0 ? prm.out.scale_g : prm.out.scale_s,
-                                      which == 0 ? prm.out.accumulate_g : prm.out.accumulate_s);
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (i0 + i + c < prm.out.in && o0 + o + r < prm.out.out)
+                prm.out.write_one(out + (size_t)(o0 + o + r) * prm.out.in + i0 + i + c, sum[r][c], scale, accumulate);
 }
 
 // delta with rows of `pitch` elements, zeros behind the last: what TMA can address where `out` is not a multiple of 16 bytes
@@ -635,7 +634,7 @@ vgc_status launch(const WgradArgs &args, const T *delta, const Checkpoint &c, vo
     VGC_CUDA_OK(launch_kernel(fn, dim3(2u * (unsigned)plan.pairs), dim3(kThreads), Ring<kParts>::kSmem, st, true, map_x, map_d, p));
     count_launch();
     if (!plan.whole && plan.pairs > 1) {
-        VGC_CUDA_OK(launch_kernel(wgrad_combine, dim3((unsigned)plan.pairs - 1, kTile / kCombineRows), dim3(256), 0, st, true, p, plan.pairs));
+        VGC_CUDA_OK(launch_kernel(wgrad_combine, dim3((unsigned)plan.pairs - 1, kTile / kCombineRows, 2), dim3(256), 0, st, true, p, plan.pairs));
         count_launch();
     }
     return VGC_OK;
