@@ -302,6 +302,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
                     __syncwarp();
                 }
             }
+            // The first block's commits arrive at both blocks' barriers, each in its own time.  None may come to shared memory that a block
+            // has given up: the last arrivals at every slot are waited for, here in both blocks (those at acc_full by the epilogue).
+            for (int i = it > R::kRaw ? it - R::kRaw : 0; ok && i < it; ++i) ok = mbar_wait(smem_u32(&raw_empty[i % R::kRaw]), (uint32_t)(i / R::kRaw) & 1u, &abort_flag, 32);
+            for (int i = it > R::kOp ? it - R::kOp : 0; ok && i < it; ++i) ok = mbar_wait(smem_u32(&op_empty[i % R::kOp]), (uint32_t)(i / R::kOp) & 1u, &abort_flag, 32);
             if (abort_flag) {                            // loads already issued must land before the block may exit
                 for (int i = it > R::kRaw ? it - R::kRaw : 0; i < it; ++i)
                     for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(&raw_full[i % R::kRaw]), (uint32_t)(i / R::kRaw) & 1u); ++n) {}
@@ -495,6 +499,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
     }
 
     // ---- common exit ----
+    if (warp == 1 && rank == 1 && abort_flag)            // where the first block's issuer gave up, too: its last commit
+        for (uint32_t n = 0; n < kWaitLimit && !mbar_try(smem_u32(drain), 0); ++n) {}
     tc_fence_before();
     __syncthreads();
     cluster_sync();                                      // the products read the other block's shared memory, too
@@ -523,8 +529,8 @@ __global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int pairs
     }
     __syncthreads();
     const int n = found[1];
+    grid_wait();                                              // (in every block: the kernel behind this one counts on it)
     if (n == 0) return;
-    grid_wait();
     int i0, o0;
     tile_at(prm, found[0], i0, o0);
     const int i = (int)(threadIdx.x & 63) * 4, o = (int)(blockIdx.y * kCombineRows + (threadIdx.x >> 6) * 4);
