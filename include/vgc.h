@@ -459,10 +459,12 @@ vgc_status vgc_layernorm_backward(const void *x, const void *dy, vgc_type type, 
  *   accumulate_*   0: written  1: added to with one fp32 addition
  *   ws             at least vgc_wgrad_checkpoint_workspace_bytes(...) bytes, 16-byte aligned; its first 32-bit word is the
  *                  status word of (1): zeroed once by the caller, VGC_DEV_TIMEOUT if a wait gave up (results invalid)
- * Every product enters exactly (bf16) or with 24 bits (fp32), sums are fp32: g within 2e-6 of the sum of the products'
- * magnitudes, S within 1e-5 of the exact sum, for |xq| and |delta| that are 0 or within [2^-50, 2^50] and sums of
- * magnitudes below 2^127 (squares and their low parts leave bf16's range beyond).  A row of delta or a column of xq with infinities or NaN gives infinities or NaN
- * there.  rows == 0: the sums are empty (cleared, or left where accumulated).  in == 0 or out == 0: no-op, OK.
+ * Every product enters exactly (bf16) or with 24 bits (fp32), sums are fp32 in a fixed order (the same inputs give the same
+ * bits): g within 2e-6 of the sum of the products' magnitudes, S within 1e-5 of the exact sum, for |xq| and |delta| that are
+ * 0 or within [2^-50, 2^50] (squares and their low parts leave bf16's range beyond) and sums of magnitudes that are 0 or
+ * within [2^-100, 2^127].  A row of delta or a column of xq with infinities or NaN gives infinities or NaN there.
+ * rows == 0: the sums are empty (cleared, or left where accumulated).  in == 0 or out == 0: no-op, OK.  rows of 2^31 - 128
+ * and more, in > 2^24, out > 2^22: VGC_ERR_INVALID_ARG.
  * ------------------------------------------------------------------------------------------- */
 size_t vgc_wgrad_checkpoint_workspace_bytes(int rows, int in, int out, vgc_type type);
 vgc_status vgc_wgrad_checkpoint(const void *checkpoint, const void *delta, vgc_type type, int rows, int in, int out,

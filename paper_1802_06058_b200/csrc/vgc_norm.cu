@@ -33,6 +33,12 @@ struct RowSum {
     float *slots;                    // [2][32 warps][N] of this group
     int warps, warp, lane, barrier, turn;
     float mine;
+    // places of warps that the row does not have: zeros (seen behind the first barrier)
+    __device__ __forceinline__ RowSum(float *slots_, int warps_, int warp_, int lane_, int barrier_)
+        : slots(slots_), warps(warps_), warp(warp_), lane(lane_), barrier(barrier_), turn(0), mine(0.f)
+    {
+        for (int i = N * warps + 32 * warp + lane; i < N * (kBlock / 32); i += 32 * warps) slots[i] = slots[32 * N + i] = 0.f;
+    }
     __device__ __forceinline__ void post(const float (&v)[N])
     {
         const bool up = lane & 16, right = lane & 8;
@@ -59,10 +65,9 @@ struct RowSum {
         if (warps > 1) {
             const float *const s = slots + 32 * N * turn + lane / kLanes;
             turn ^= 1;
-            m = 0.f;
+            m = s[N * (lane % kLanes)];
 #pragma unroll
-            for (int w = 0; w < kBlock / 32; w += kLanes)
-                if (w < warps) m += w + lane % kLanes < warps ? s[N * (w + lane % kLanes)] : 0.f;
+            for (int w = kLanes; w < kBlock / 32; w += kLanes) m += s[N * (w + lane % kLanes)];
 #pragma unroll
             for (int d = kLanes / 2; d >= 1; d >>= 1) m += __shfl_xor_sync(~0u, m, d);
         }
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
     extern __shared__ uint4 dynamic[];
     __shared__ float slots[8][128];
     const int lane = threadIdx.x & 31, all = threadIdx.x >> 5, group = all / p.warps, warp = all - group * p.warps;
-    RowSum<2> sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
+    RowSum<2> sum(slots[group], p.warps, warp, lane, 1 + group);
     grid_release();
     grid_wait();
     const int C = p.features, first = warp * kParts * kSeg;
@@ -400,7 +405,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
     __shared__ float slots[8][128 * kAt];
     __shared__ float joined[kParts == 1 ? 8 * kSeg : 1];      // column sums of a block's groups: groups * warps <= 8
     const int lane = threadIdx.x & 31, all = threadIdx.x >> 5, group = all / p.warps, warp = all - group * p.warps;
-    RowSum<2 * kAt> sum = {slots[group], p.warps, warp, lane, 1 + group, 0, 0.f};
+    RowSum<2 * kAt> sum(slots[group], p.warps, warp, lane, 1 + group);
     grid_release();
     grid_wait();
     const int C = p.features, first = (kWide ? blockIdx.y * kSeg : 0) + warp * kParts * kSeg;
@@ -436,24 +441,26 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
         step = kMode == kSamples ? 1 : each;
         jump = kMode == kSamples ? (each - 1) * p.per_example : 0;              // over the other groups' samples
     }
-    // what moves from row to row: an index, and how many rows of its sample are left behind it
+    // what moves from row to row: a distance in bytes, and how many rows of its sample are left behind it
     struct Cursor {
-        uint32_t row;                                         // (steps past the last row: 2^31 rows and more)
+        uint64_t at;
         int left;
-        __device__ __forceinline__ void next(int step, int jump, int per)
+        __device__ __forceinline__ void next(uint64_t step, uint64_t jump, int per)
         {
-            row += (uint32_t)step;
+            at += step;
             if constexpr (kMode == kSamples) {
                 if (left == 0) {
-                    row += (uint32_t)jump;
+                    at += jump;
                     left = per;
                 }
                 --left;
             }
         }
     };
-    const Cursor start = {(uint32_t)row, p.per_example - 1};
-    Cursor ahead = start, here = start;
+    const uint64_t row_bytes = (uint64_t)C * sizeof(T), on = (uint64_t)step * row_bytes, over = (uint64_t)jump * row_bytes;
+    Cursor ahead = {(uint64_t)row * row_bytes, p.per_example - 1}, here = ahead, numbers = {(uint64_t)row * sizeof(float), p.per_example - 1};
+    const char *const from_x = reinterpret_cast<const char *>(p.x + first), *const from_dy = reinterpret_cast<const char *>(p.dy + first);
+    char *const to_dx = reinterpret_cast<char *>(p.dx + first);
     const float per = 1.f / (float)C;
     R rows(dynamic, C - first, lane);
     int asked = 0;
@@ -462,24 +469,25 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
     float2 next_sums[kAt] = {};
     auto ask = [&]() {
         if (asked < count) {
-            const size_t at = (size_t)ahead.row * C + first;
-            rows.ask(0, p.x + at);
-            rows.ask(1, p.dy + at);
-            ahead.next(step, jump, p.per_example);
+            rows.ask(0, reinterpret_cast<const T *>(from_x + ahead.at));
+            rows.ask(1, reinterpret_cast<const T *>(from_dy + ahead.at));
+            ahead.next(on, over, p.per_example);
         }
         ++asked;
         rows.asked();
     };
-    Cursor numbers = start;
     int numbered = 0;
     auto ask_numbers = [&]() {
 #pragma unroll
         for (int at = 0; at < kAt; ++at)
             if (numbered + at < count) {
-                next_mean[at] = ld_f(p.mean + numbers.row);
-                next_rstd[at] = ld_f(p.rstd + numbers.row);
-                if constexpr (kWide) next_sums[at] = make_float2(ld_f(&p.row_sums[numbers.row].x), ld_f(&p.row_sums[numbers.row].y));
-                numbers.next(step, jump, p.per_example);
+                next_mean[at] = ld_f(reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.mean) + numbers.at));
+                next_rstd[at] = ld_f(reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.rstd) + numbers.at));
+                if constexpr (kWide) {
+                    const float *const two = reinterpret_cast<const float *>(reinterpret_cast<const char *>(p.row_sums) + 2 * numbers.at);
+                    next_sums[at] = make_float2(ld_f(two), ld_f(two + 1));
+                }
+                numbers.next((uint64_t)step * sizeof(float), (uint64_t)jump * sizeof(float), p.per_example);
             }
         numbered += kAt;
     };
@@ -537,7 +545,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
                 }
             if constexpr (kMode == kSamples) {
                 const bool last = this_row.left == 0 && i + at < count;
-                this_row.next(step, jump, p.per_example);
+                this_row.next(on, over, p.per_example);
                 if (last) {
 #pragma unroll
                     for (int k = 0; k < kParts; ++k)
@@ -586,7 +594,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
         for (int at = 0; at < kAt; ++at) {
             if (kAt > 1 && i + at >= count) break;
             const F2 less = f2(-v[2 * at]), by = f2(-v[2 * at + 1]);
-            T *const to = p.dx + (size_t)here.row * C + first;
+            T *const to = reinterpret_cast<T *>(to_dx + here.at);
 #pragma unroll
             for (int k = 0; k < kParts; ++k) {
                 Raw<T> out;
@@ -604,7 +612,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
                 }
                 store_seg<kVec>(to + k * kSeg, C - first - k * kSeg, lane, out);
             }
-            here.next(step, jump, p.per_example);
+            here.next(on, over, p.per_example);
         }
     }
 
@@ -658,7 +666,7 @@ __global__ void __launch_bounds__(512) norm_row_sums(const Backward<T> p, float2
 {
     __shared__ float slots[128];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5, C = p.features;
-    RowSum<2> sum = {slots, warps, warp, lane, 1, 0, 0.f};
+    RowSum<2> sum(slots, warps, warp, lane, 1);
     grid_release();
     grid_wait();
     for (long long row = blockIdx.x; row < p.rows; row += gridDim.x) {
