@@ -692,7 +692,7 @@ __global__ void __launch_bounds__(512) norm_row_sums(const Backward<T> p, float2
     }
 }
 
-// The blocks' partial sums of 32 features, each of 16 warps a sixteenth of them, added in order.
+// The blocks' partial sums of 32 features, each of 32 warps a part of them, added in order.
 // samples == 0: partial [n][4][C].  Otherwise [samples][pieces][2][C]: a sample's pieces are added, then squared.
 struct Combine {
     const float *partial;
@@ -701,7 +701,7 @@ struct Combine {
     int accumulate_g, accumulate_s;
     float *out[4];                   // g_gamma, g_beta, s_gamma, s_beta
 };
-constexpr int kCombineWarps = 16;
+constexpr int kCombineWarps = 32;
 __global__ void __launch_bounds__(32 * kCombineWarps) norm_combine(const Combine p)
 {
     __shared__ float part[4][kCombineWarps][32];
@@ -721,7 +721,7 @@ __global__ void __launch_bounds__(32 * kCombineWarps) norm_combine(const Combine
             const int each = (p.samples + kCombineWarps - 1) / kCombineWarps, last = min(p.samples, (warp + 1) * each);
             for (int s = warp * each; s < last; ++s) {
                 float a = 0.f, b = 0.f;
-#pragma unroll 4
+#pragma unroll 8
                 for (int i = 0; i < p.pieces; ++i) {
                     const float *const at = p.partial + ((size_t)s * p.pieces + i) * 2 * C + c;
                     a += ld_f(at);
