@@ -830,6 +830,31 @@ def profile_kernels():
         vgc.vgc_unpack_indices(packed, out.counters[0:1], back, status)
     torch.cuda.synchronize()
     print(json.dumps({"case": "pack_indices + unpack_indices", "words": c["nnz"], "packed_bytes": int(nbytes.item())}))
+    # layer norm, 8-bit checkpoints, a linear layer's gradient and statistic (activations of 67 - 268 MB)
+    for rows, C, dtype, per in ((16384, 4096, torch.bfloat16, 1), (8192, 8192, torch.bfloat16, 1), (16384, 1001, torch.float32, 1), (12608, 1280, torch.bfloat16, 197)):
+        x = torch.randn(rows, C, device=dev).to(dtype); y = torch.empty_like(x)
+        gamma, beta, mean, rstd = torch.ones(C, device=dev), torch.zeros(C, device=dev), torch.empty(rows, device=dev), torch.empty(rows, device=dev)
+        ckpt = torch.empty(vgc.vgc_checkpoint_bytes(rows, C), dtype=torch.uint8, device=dev)
+        ws = torch.empty(vgc.vgc_layernorm_backward_workspace_bytes(rows, C, per), dtype=torch.uint8, device=dev)
+        sums = [torch.empty(C, device=dev) for _ in range(4)]
+        for _ in range(2):
+            vgc.vgc_layernorm(x, gamma, beta, 1e-5, y, mean, rstd)
+            vgc.vgc_layernorm(x, gamma, beta, 1e-5, y, mean, rstd, checkpoint=ckpt)
+            vgc.vgc_layernorm_backward(x, y, gamma, mean, rstd, y, *sums, rows_per_example=per, ws=ws)
+            vgc.vgc_checkpoint_store(x, ckpt)
+            vgc.vgc_checkpoint_load(ckpt, x)
+        torch.cuda.synchronize()
+        print(json.dumps({"case": "layernorm, with checkpoint, backward; checkpoint store, load", "rows": rows, "features": C, "dtype": str(dtype),
+                          "rows_per_example": per}))
+    for rows, n_in, n_out, dtype in ((8192, 1024, 1024, torch.bfloat16), (3001, 1000, 2051, torch.float32)):
+        ckpt = vgc.vgc_checkpoint_store(torch.randn(rows, n_in, device=dev), torch.empty(vgc.vgc_checkpoint_bytes(rows, n_in), dtype=torch.uint8, device=dev))
+        d = torch.randn(rows, n_out, device=dev).to(dtype)
+        G, S = torch.empty(n_out, n_in, device=dev), torch.empty(n_out, n_in, device=dev)
+        ws = torch.zeros(vgc.vgc_wgrad_checkpoint_workspace_bytes(rows, n_in, n_out, dtype), dtype=torch.uint8, device=dev)
+        for _ in range(2):
+            vgc.vgc_wgrad_checkpoint(ckpt, d, G, S, ws=ws)
+        torch.cuda.synchronize()
+        print(json.dumps({"case": "wgrad_checkpoint", "rows": rows, "in": n_in, "out": n_out, "dtype": str(dtype)}))
 
 
 # ----------------------------------------------------------------------------------------------

@@ -1,17 +1,26 @@
 // Layer norm over the rows of an activation matrix, its backward pass, and the gradient and squared-gradient sums of gain and bias.
 //
-// Forward: a row stays in the registers of its warps (8 features a lane, 16 beyond 8192) between the mean, the squared deviations
-// from it and the write: one read and one write of the matrix, no cancellation in the variance.
+// Forward: a row stays in the registers of its warps (8, 16 or 32 features a lane) between the mean, the squared deviations from it
+// and the write: one read and one write of the matrix, no cancellation in the variance.
 // Backward: dx = rstd (w - mean(w) - xh mean(w xh)), w = dy gamma.  The same lanes keep the column sums of their features (dy xh, dy
-// and their squares) in registers over all rows that their block takes, so x and dy are read once; each block leaves one row of
-// partial sums, which norm_combine adds in the blocks' order.
-//   samples of one row      four sums per feature
+// and their squares) over all rows that their block takes, so x and dy are read once; each block leaves one row of partial sums,
+// which norm_combine adds in the blocks' order.
+//   samples of one row      four sums per feature (the squares' in shared memory where a lane has 16 features)
 //   samples of many rows    whole samples where there are enough of them for every group of warps (the sample's sums, squared
 //                           when it ends, beside the four), otherwise pieces of samples: a block's two sums belong to one sample, and
 //                           norm_combine squares what a sample's pieces add up to
 // Beyond 8192 features a block has no registers for a row's column sums: norm_row_sums finds the two means of every row first, and
 // blocks of 256 columns need no sums across a row (x and dy are read twice).
-// Bound: HBM.
+// Rows come in by asynchronous copies, up to eight of them under way; arithmetic is on packed pairs of fp32.
+// Sums, means and statistics are fp32; y and dx are rounded to their type once.
+// Bound: instructions and the wait for a row's sums in bf16, HBM in fp32.  Measured (B200, one call among others, of the measured copy
+// rate): forward 16384 x 4096 bf16 50 us (0.83), fp32 98 us (0.85), with the checkpoint 87 us (0.60) and 125 (0.75); 16384 x 16384 bf16
+// 302 us (0.55).  Backward 16384 x 4096 bf16 93 us (0.67), samples of 2048 rows 83 us (0.75), of 8 rows 107 (0.58); 8192 x 8192 bf16 134 us
+// (0.47), fp32 145 us (0.86); 65536 x 1024 bf16 82 us (0.76); 4096 x 16384, read twice, 173 us (0.36).
+// The first form (rows loaded into registers one ahead, one fp32 at a time) took 91 us forward, 121 backward (16384 x 4096 bf16).  Tried
+// and dropped: a step's sums waited for a step later (backward 97 -> 111 us: the rows held meanwhile cost moves), two blocks an SM with
+// 64 registers a thread (200 us: spills), the two-pass form from 4096 features on (8192 x 8192: 180 -> 185 us), 8 instead of
+// 16 features a lane in the forward pass (bf16, with the checkpoint: 88 -> 102 us).
 #include <cfloat>
 #include <type_traits>
 

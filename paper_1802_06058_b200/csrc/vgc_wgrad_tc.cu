@@ -19,7 +19,14 @@
 // every pair takes an equal stretch of the sequence, leaves the tiles it shares with its neighbours as partial sums, and
 // wgrad_combine adds those in the pairs' order.
 // Bound: shared memory and power.  A block's six products of a slice (bf16) take 384 cycles of the tensor pipe; their operands, 36 KB, the
-// transform's 32 KB and TMA's 8 KB take 608 at 128 bytes a cycle.  (Single blocks of 128 x 128: 48 + 44 + 12 KB, 832 cycles.)
+// transform's 32 KB and TMA's 8 KB take 608 at 128 bytes a cycle, and a slice takes 625.  (Single blocks of 128 x 128: 48 + 44 + 12 KB, 832
+// cycles.)  The clock is at 1.55 GHz meanwhile, under the power cap.
+// Measured (B200, one call among others; rate: the products issued): 16384 x 4096 -> 16384 bf16 6.1 ms, 1080 TFLOP/s (0.77 of the measured
+// sustained bf16 rate); 8192 x 1024 -> 1024 bf16 57 us; 3001 x 1000 -> 2051 fp32 90 us, 410 TFLOP/s on 111 % of the tiles' area; 128 x 784 ->
+// 1024 fp32 9.5 us.  On the way (16384 x 4096 -> 16384): CUDA cores 139.7 ms; single blocks 8.3; one elected lane of a converged warp as
+// the issuer 6.9 (issued under a lane test, every product took 150 cycles instead of 64); pairs 6.3.  An arrival at the other block's barrier
+// with .release.cluster took so long that pairs were slower than single blocks (9.4 ms): the operands are made visible by the proxy
+// fence, and the plain arrival is enough.
 #include "vgc_tc.cuh"
 #include "vgc_wgrad.cuh"
 
@@ -493,7 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) wgrad_t
                 }
             } else {                                     // behind the tile's beginning: the pair's first stretch; else its last
                 float *const to = prm.partial + ((size_t)(2 * (blockIdx.x >> 1) + (walk.s0 > 0 ? 0 : 1)) * 2 + which) * kPartial + i;
-                write_column<false>(sum, to, kTileI * sizeof(float), kTile, 1.f);
+                if (i0 + i < prm.out.in) write_column<false>(sum, to, kTileI * sizeof(float), prm.out.out - o0, 1.f);
             }
         }
     }
@@ -537,9 +544,9 @@ __global__ void __launch_bounds__(256) wgrad_combine(const Params prm, int pairs
     float *const out = blockIdx.z == 0 ? prm.out.g : prm.out.S;
     const float scale = blockIdx.z == 0 ? prm.out.scale_g : prm.out.scale_s;
     const int accumulate = blockIdx.z == 0 ? prm.out.accumulate_g : prm.out.accumulate_s;
-    if (!out) return;
+    if (!out || i0 + i >= prm.out.in || o0 + o >= prm.out.out) return;      // (past the edges nothing was left, nor is it written)
     float sum[4][4];
-#pragma unroll 2
+#pragma unroll 4
     for (int k = 0; k < n; ++k) {                             // the first pair's last stretch, the others' first
         const float *const from = prm.partial + ((size_t)(2 * ((int)blockIdx.x + k) + (k == 0 ? 1 : 0)) * 2 + blockIdx.z) * kPartial + o * kTileI + i;
 #pragma unroll
@@ -585,7 +592,14 @@ Plan plan_of(int rows, int in, int out, vgc_type type)
     const long long rounds = (tiles + kMost - 1) / kMost;
     p.whole = rounds * (p.slices + kPerTile) <= (total + kMost - 1) / kMost + kPerTile * ((tiles + kMost - 1) / kMost) + kCut;
     if (p.whole) p.pairs = (int)((tiles + rounds - 1) / rounds);
-    else p.pairs = total < kMost ? (int)total : kMost;
+    else {
+        // Parts of a tile are worked on side by side, but added one after another, a part in about two thirds of a slice's time: the sum of
+        // both is least for sqrt(3/2 slices) parts (one tile of 41 slices, fp32: in 41 parts 28.7 us, in 8 14.0).
+        int parts = 1;
+        while ((long long)parts * parts * 2 < 3LL * p.slices && parts < kMost) ++parts;
+        p.pairs = (int)(tiles * parts < kMost ? tiles * parts : kMost);
+        if (p.pairs > total) p.pairs = (int)total;
+    }
     p.partial_bytes = p.whole ? 0 : (size_t)p.pairs * 2 * 2 * kPartial * sizeof(float);
     const int item = type == VGC_FP32 ? 4 : 2;
     p.pitch = (int)round_up((size_t)out, 16 / item);
