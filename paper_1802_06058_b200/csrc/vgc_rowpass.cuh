@@ -242,6 +242,14 @@ __device__ __forceinline__ uint32_t e4m3_pair(F2 v)
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(q) : "f"(hi_of(v)), "f"(lo_of(v)));
     return q;
 }
+// four, in the order of their bytes
+__device__ __forceinline__ uint32_t e4m3_quad(F2 a, F2 b)
+{
+    uint32_t q;
+    asm("{\n\t.reg .b16 l, u;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %1, %2;\n\tcvt.rn.satfinite.e4m3x2.f32 u, %3, %4;\n\tmov.b32 %0, {l, u};\n\t}"
+        : "=r"(q) : "f"(hi_of(a)), "f"(lo_of(a)), "f"(hi_of(b)), "f"(lo_of(b)));
+    return q;
+}
 // v - v is 0, or NaN where v is infinite or NaN
 __device__ __forceinline__ F2 infinity_to_nan(F2 v) { return add2(v, fma2(v, f2(-1.f), v)); }
 // two codes as numbers (exact)
@@ -286,8 +294,8 @@ __device__ __forceinline__ void store_blocks(const Checkpoint &c, int row, int f
         word |= __shfl_xor_sync(~0u, word, 8);
         if (8 * lane < left) {
             uint2 q;
-            q.x = e4m3_pair(mul2(v[0], inverse)) | e4m3_pair(mul2(v[1], inverse)) << 16;
-            q.y = e4m3_pair(mul2(v[2], inverse)) | e4m3_pair(mul2(v[3], inverse)) << 16;
+            q.x = e4m3_quad(mul2(v[0], inverse), mul2(v[1], inverse));
+            q.y = e4m3_quad(mul2(v[2], inverse), mul2(v[3], inverse));
             *reinterpret_cast<uint2 *>(codes + 8 * lane) = q;
             if ((lane & 15) == 0) *scale_word(c, row, unit + (lane >> 4)) = word;
         }
@@ -304,7 +312,7 @@ __device__ __forceinline__ void store_blocks(const Checkpoint &c, int row, int f
             word |= __shfl_xor_sync(~0u, word, 8);
             word |= __shfl_xor_sync(~0u, word, 16);
             if (128 * j < left) {
-                *reinterpret_cast<uint32_t *>(codes + 128 * j + 4 * lane) = e4m3_pair(mul2(v[2 * j], inverse)) | e4m3_pair(mul2(v[2 * j + 1], inverse)) << 16;
+                *reinterpret_cast<uint32_t *>(codes + 128 * j + 4 * lane) = e4m3_quad(mul2(v[2 * j], inverse), mul2(v[2 * j + 1], inverse));
                 if (lane == 0) *scale_word(c, row, unit + j) = word;
             }
         }

@@ -572,6 +572,7 @@ __global__ void __launch_bounds__(256) wgrad_repack(const T *delta, T *to, int r
     grid_release();
     grid_wait();
     for (long long row = blockIdx.x; row < rows; row += gridDim.x)
+#pragma unroll 8
         for (int c = threadIdx.x; c < pitch; c += 256) to[row * pitch + c] = c < out ? delta[row * out + c] : T(0.f);
 }
 
