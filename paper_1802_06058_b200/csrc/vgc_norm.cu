@@ -87,28 +87,29 @@ struct RowSum {
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// How rows come into a block: kDepth of them under way in shared memory (rows that do not start on 16 bytes: one, in registers).
-// kArrays matrices are read.
+// How rows come into a block: kDepth of them under way in shared memory, in pieces of 16 bytes, or of 4 where fp32 rows do not start on
+// 16 (bf16 rows that do not: one, in registers).  kArrays matrices are read.
 template <class T, bool kVec, int kParts, int kArrays>
 struct Rows {
-    static constexpr int kPieces = kPieces16<T>;
-    static constexpr uint32_t kRow = 16 * kPieces * kParts * kArrays;                     // bytes a thread
-    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kVec ? 1 : kFit > 8 ? 8 : kFit < 3 && kArrays == 1 ? 3 : kFit;
-    __host__ __device__ static constexpr uint32_t smem(int threads) { return kVec ? kRow * kDepth * threads : 0; }
-    Raw<T> ahead[kVec ? 1 : kArrays][kVec ? 1 : kParts];
+    static constexpr bool kRing = kVec || sizeof(T) == 4;
+    static constexpr int kPieces = kVec ? kPieces16<T> : 8, kPiece = kVec ? 16 : 4, kLaneOwn = kVec ? kPieces : 1;
+    static constexpr uint32_t kRow = 16 * kPieces16<T> * kParts * kArrays;               // bytes a thread
+    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kRing ? 1 : kFit > 8 ? 8 : kFit < 3 && kArrays == 1 ? 3 : kFit;
+    __host__ __device__ static constexpr uint32_t smem(int threads) { return kRing ? kRow * kDepth * threads : 0; }
+    Raw<T> ahead[kRing ? 1 : kArrays][kRing ? 1 : kParts];
     uint32_t begin, end, at, pitch;  // the ring of this thread's pieces, the row taken next
-    uint32_t offset[kParts][kPieces], bytes[kParts][kPieces];       // this lane's pieces of a warp's features; 0 past the row's end
+    uint32_t offset[kParts][kLaneOwn], bytes[kParts][kLaneOwn];       // this lane's pieces of a warp's features; 0 past the row's end
     int left, lane;
     // left: features of a row from the warp's first one on
     __device__ __forceinline__ Rows(void *dynamic, int left_, int lane_) : left(left_), lane(lane_)
     {
-        pitch = 16 * blockDim.x;
-        at = begin = smem_at(dynamic) + 16 * threadIdx.x;
-        end = begin + pitch * (kRow / 16) * kDepth;
+        pitch = kPiece * blockDim.x;
+        at = begin = smem_at(dynamic) + kPiece * threadIdx.x;
+        end = begin + pitch * (kRow / kPiece) * kDepth;
 #pragma unroll
         for (int k = 0; k < kParts; ++k)
 #pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
+            for (int j = 0; j < kLaneOwn; ++j) {
                 const int c = k * kSeg + (sizeof(T) == 2 ? 8 * lane : 128 * j + 4 * lane);
                 bytes[k][j] = c < left ? 16 : 0;
                 offset[k][j] = c < left ? c * (int)sizeof(T) : 0;
@@ -123,6 +124,12 @@ struct Rows {
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j)
                     copy_16(at + pitch * ((array * kParts + k) * kPieces + j), reinterpret_cast<const char *>(row) + offset[k][j], bytes[k][j]);
+            } else if constexpr (kRing) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int c = k * kSeg + 32 * i + lane;
+                    copy_4(at + pitch * ((array * kParts + k) * kPieces + i), row + (c < left ? c : 0), c < left ? 4 : 0);
+                }
             } else {
                 load_seg<false>(row + k * kSeg, left - k * kSeg, lane, ahead[array][k]);
             }
@@ -130,22 +137,28 @@ struct Rows {
     }
     __device__ __forceinline__ void asked()                   // (or nothing was left to ask for)
     {
-        if constexpr (kVec) {
+        if constexpr (kRing) {
             copies_commit();
-            at += pitch * (kRow / 16);
+            at += pitch * (kRow / kPiece);
             at = at == end ? begin : at;
         }
     }
     __device__ __forceinline__ void arrived() const
     {
-        if constexpr (kVec) copies_wait<kDepth - 1>();
+        if constexpr (kRing) copies_wait<kDepth - 1>();
     }
     __device__ __forceinline__ void take(int array, Raw<T> (&x)[kParts])
     {
 #pragma unroll
         for (int k = 0; k < kParts; ++k) {
-            if constexpr (kVec) take_seg(at + pitch * (array * kParts + k) * kPieces, pitch, x[k]);
-            else x[k] = ahead[array][k];
+            if constexpr (kVec) {
+                take_seg(at + pitch * (array * kParts + k) * kPieces, pitch, x[k]);
+            } else if constexpr (kRing) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[k].v[i] = ld_shared_f(at + pitch * ((array * kParts + k) * kPieces + i));
+            } else {
+                x[k] = ahead[array][k];
+            }
         }
     }
 };
@@ -336,7 +349,7 @@ vgc_status forward_as(const void *x, const float *gamma, const float *beta, int 
         constexpr bool kVec = decltype(vector)::value;
         using R = Rows<T, kVec, kParts, 1>;
         const auto fn = checkpoint ? norm_forward<T, kVec, kParts, true> : norm_forward<T, kVec, kParts, false>;
-        if (kVec) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
+        if (R::kRing) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
         VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)(need < resident ? need : resident)), dim3((unsigned)threads), R::smem(threads), st, true, p));
         count_launch();
         return VGC_OK;
@@ -784,7 +797,7 @@ vgc_status backward_as(const void *x, const void *dy, const float *gamma, const 
         const auto fn = norm_backward<T, kVec, kParts, decltype(mode)::value, decltype(wide)::value>;
         constexpr int kOwn = kParts > 1 && decltype(mode)::value == kRows ? 64 * kParts : 0;      // bytes a thread: its sums of squares
         static_assert(R::smem(kBlock) + kOwn * kBlock + 16384 <= 232448, "");
-        if (kVec || kOwn) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock) + kOwn * kBlock));
+        if (R::kRing || kOwn) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock) + kOwn * kBlock));
         VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks, plan.wide ? (unsigned)((features + kSeg - 1) / kSeg) : 1u), dim3((unsigned)threads),
                                   R::smem(threads) + kOwn * threads, st, true, p));
         count_launch();

@@ -178,6 +178,16 @@ __device__ __forceinline__ void copy_16(uint32_t smem, const void *from, uint32_
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem), "l"(from), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void copy_4(uint32_t smem, const void *from, uint32_t bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ float ld_shared_f(uint32_t smem)
+{
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(smem) : "memory");
+    return v;
+}
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 __device__ __forceinline__ uint4 ld_shared_16(uint32_t smem)
