@@ -57,7 +57,6 @@ __global__ void __launch_bounds__(kThreads) checkpoint_store(const T *x, int row
     }
 }
 
-// kVec: a lane takes 8 neighbouring features in bf16, twice 4 in fp32; otherwise single ones, as in the store
 template <class T, bool kVec>
 __global__ void __launch_bounds__(kThreads) checkpoint_load(T *x, int rows, int features, uint32_t segs, Checkpoint c)
 {
@@ -73,7 +72,7 @@ __global__ void __launch_bounds__(kThreads) checkpoint_load(T *x, int rows, int 
             const int first = (int)ahead.seg * kSeg, left = c.wide - first, unit = first >> 7;
             const uint8_t *const codes = c.codes + (size_t)ahead.row * c.wide + first;
             q[k][0] = q[k][1] = 0;
-            if constexpr (kVec && sizeof(T) == 2) {
+            if constexpr (sizeof(T) == 2) {
                 if (8 * lane < left) {
                     const uint2 v = *reinterpret_cast<const uint2 *>(codes + 8 * lane);
                     q[k][0] = v.x; q[k][1] = v.y;
@@ -103,8 +102,8 @@ __global__ void __launch_bounds__(kThreads) checkpoint_load(T *x, int rows, int 
                 float a, b;
                 e4m3_values(q[k][j >> 1] >> (16 * (j & 1)), a, b);
                 F2 scale;
-                if constexpr (!kVec) scale = f2(scale_of(w[k][j >> 1] >> (16 * (j & 1)) & 255u), scale_of(w[k][j >> 1] >> (16 * (j & 1) + 8) & 255u));
-                else if constexpr (sizeof(T) == 2) scale = f2(scale_of(w[k][0] >> (8 * ((lane >> 2) & 3)) & 255u));
+                if constexpr (sizeof(T) == 2) scale = f2(scale_of(w[k][0] >> (8 * ((lane >> 2) & 3)) & 255u));
+                else if constexpr (!kVec) scale = f2(scale_of(w[k][j >> 1] >> (16 * (j & 1)) & 255u), scale_of(w[k][j >> 1] >> (16 * (j & 1) + 8) & 255u));
                 else scale = f2(scale_of(w[k][j >> 1] >> (8 * (lane >> 3)) & 255u));
                 set_pair(out, j, mul2(f2(a, b), scale));
             }

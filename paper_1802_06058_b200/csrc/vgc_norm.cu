@@ -87,25 +87,37 @@ struct RowSum {
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
-// How rows come into a block: kDepth of them under way in shared memory, in pieces of 16 bytes, or of 4 where fp32 rows do not start on
-// 16 (bf16 rows that do not: one, in registers).  kArrays matrices are read.
+// How rows come into a block: kDepth of them under way in shared memory.  kArrays matrices are read.
+//   kVec          rows start on 16 bytes: every thread copies the pieces of 16 bytes that it takes itself
+//   fp32          otherwise: the same in pieces of 4
+//   bf16          otherwise: a warp copies the aligned pieces, 33 of them, that hold its 256 features, and how far the first feature is into
+//                 them, to a place of its own; a lane takes its 16 bytes from two neighbouring pieces
 template <class T, bool kVec, int kParts, int kArrays>
 struct Rows {
-    static constexpr bool kRing = kVec || sizeof(T) == 4;
+    static constexpr bool kShifted = !kVec && sizeof(T) == 2;
     static constexpr int kPieces = kVec ? kPieces16<T> : 8, kPiece = kVec ? 16 : 4, kLaneOwn = kVec ? kPieces : 1;
-    static constexpr uint32_t kRow = 16 * kPieces16<T> * kParts * kArrays;               // bytes a thread
-    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = !kRing ? 1 : kFit > 8 ? 8 : kFit < 3 && kArrays == 1 ? 3 : kFit;
-    __host__ __device__ static constexpr uint32_t smem(int threads) { return kRing ? kRow * kDepth * threads : 0; }
-    Raw<T> ahead[kRing ? 1 : kArrays][kRing ? 1 : kParts];
-    uint32_t begin, end, at, pitch;  // the ring of this thread's pieces, the row taken next
+    static constexpr uint32_t kWarpPlace = 544;               // 33 pieces, the distance
+    static constexpr uint32_t kRow = 16 * kPieces16<T> * kParts * kArrays;                // bytes a thread
+    static constexpr int kFit = 131072 / (kRow * kBlock), kDepth = kFit > 8 ? 8 : kFit < 3 && kArrays == 1 ? 3 : kFit;
+    __host__ __device__ static constexpr uint32_t smem(int threads)
+    {
+        return kShifted ? threads / 32 * kWarpPlace * kParts * kArrays * kDepth : kRow * kDepth * threads;
+    }
+    uint32_t begin, end, at, pitch;  // the ring of this thread's pieces (of this warp's places), the row taken next
     uint32_t offset[kParts][kLaneOwn], bytes[kParts][kLaneOwn];       // this lane's pieces of a warp's features; 0 past the row's end
     int left, lane;
     // left: features of a row from the warp's first one on
     __device__ __forceinline__ Rows(void *dynamic, int left_, int lane_) : left(left_), lane(lane_)
     {
-        pitch = kPiece * blockDim.x;
-        at = begin = smem_at(dynamic) + kPiece * threadIdx.x;
-        end = begin + pitch * (kRow / kPiece) * kDepth;
+        if constexpr (kShifted) {
+            pitch = kWarpPlace;
+            at = begin = smem_at(dynamic) + (threadIdx.x >> 5) * kWarpPlace * kParts * kArrays * kDepth;
+            end = begin + kWarpPlace * kParts * kArrays * kDepth;
+        } else {
+            pitch = kPiece * blockDim.x;
+            at = begin = smem_at(dynamic) + kPiece * threadIdx.x;
+            end = begin + pitch * (kRow / kPiece) * kDepth;
+        }
 #pragma unroll
         for (int k = 0; k < kParts; ++k)
 #pragma unroll
@@ -124,28 +136,35 @@ struct Rows {
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j)
                     copy_16(at + pitch * ((array * kParts + k) * kPieces + j), reinterpret_cast<const char *>(row) + offset[k][j], bytes[k][j]);
-            } else if constexpr (kRing) {
+            } else if constexpr (!kShifted) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int c = k * kSeg + 32 * i + lane;
                     copy_4(at + pitch * ((array * kParts + k) * kPieces + i), row + (c < left ? c : 0), c < left ? 4 : 0);
                 }
             } else {
-                load_seg<false>(row + k * kSeg, left - k * kSeg, lane, ahead[array][k]);
+                const uint32_t place = at + pitch * (array * kParts + k), off = (uint32_t)reinterpret_cast<uintptr_t>(row) & 15u;      // (a segment is 512 bytes)
+                const char *const base = reinterpret_cast<const char *>(row) - off;
+                const int whole = (int)off + 2 * left - 512 * k;                          // bytes from the first piece to the row's end
+                const int mine = min(max(whole - 16 * lane, 0), 16), past = off ? min(max(whole - 512, 0), 16) : 0;
+                copy_16(place + 16 * lane, base + (mine ? 512 * k + 16 * lane : 0), (uint32_t)mine);
+                if (lane == 0) {
+                    copy_16(place + 512, base + (past ? 512 * (k + 1) : 0), (uint32_t)past);
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(place + 528), "r"(off) : "memory");
+                }
             }
         }
     }
     __device__ __forceinline__ void asked()                   // (or nothing was left to ask for)
     {
-        if constexpr (kRing) {
-            copies_commit();
-            at += pitch * (kRow / kPiece);
-            at = at == end ? begin : at;
-        }
+        copies_commit();
+        at += kShifted ? pitch * kParts * kArrays : pitch * (kRow / kPiece);
+        at = at == end ? begin : at;
     }
     __device__ __forceinline__ void arrived() const
     {
-        if constexpr (kRing) copies_wait<kDepth - 1>();
+        copies_wait<kDepth - 1>();
+        if constexpr (kShifted) __syncwarp();                 // what the other lanes asked for, too
     }
     __device__ __forceinline__ void take(int array, Raw<T> (&x)[kParts])
     {
@@ -153,13 +172,16 @@ struct Rows {
         for (int k = 0; k < kParts; ++k) {
             if constexpr (kVec) {
                 take_seg(at + pitch * (array * kParts + k) * kPieces, pitch, x[k]);
-            } else if constexpr (kRing) {
+            } else if constexpr (!kShifted) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[k].v[i] = ld_shared_f(at + pitch * ((array * kParts + k) * kPieces + i));
             } else {
-                x[k] = ahead[array][k];
+                const uint32_t place = at + pitch * (array * kParts + k);
+                const uint4 v = bytes_from(ld_shared_16(place + 16 * lane), ld_shared_16(place + 16 * lane + 16), __float_as_uint(ld_shared_f(place + 528)));
+                x[k].v[0] = v.x; x[k].v[1] = v.y; x[k].v[2] = v.z; x[k].v[3] = v.w;
             }
         }
+        if constexpr (kShifted) __syncwarp();                 // all have it: the place may be asked into
     }
 };
 
@@ -349,7 +371,7 @@ vgc_status forward_as(const void *x, const float *gamma, const float *beta, int 
         constexpr bool kVec = decltype(vector)::value;
         using R = Rows<T, kVec, kParts, 1>;
         const auto fn = checkpoint ? norm_forward<T, kVec, kParts, true> : norm_forward<T, kVec, kParts, false>;
-        if (R::kRing) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
+        VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock)));
         VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)(need < resident ? need : resident)), dim3((unsigned)threads), R::smem(threads), st, true, p));
         count_launch();
         return VGC_OK;
@@ -413,14 +435,14 @@ struct Backward {
     int per_example, pieces, length;
 };
 
-// kAt rows at a time, so that the wait for their sums over the row is shared.  (fp32 rows of single elements and 16 features a lane have
+// kAt rows at a time, so that the wait for their sums over the row is shared.  (16 features a lane have
 // no registers for two.)  A lane keeps the rows' dy and xh between the sums and the write, or, where it has 16 features, the rows
 // themselves.
 template <class T, bool kVec, int kParts, int kMode, bool kWide>
 __global__ void __launch_bounds__(kBlock, 1) norm_backward(const Backward<T> p)
 {
     using R = Rows<T, kVec, kParts, 2>;
-    constexpr int kAt = kVec && kParts == 1 ? 2 : 1;
+    constexpr int kAt = kParts == 1 ? 2 : 1;
     constexpr bool kShared = kParts > 1 && kMode == kRows;    // the sums of squares lie in shared memory, every thread's own
     constexpr bool kAgain = kParts > 1;      // xh worked out again for the write
     extern __shared__ uint4 dynamic[];
@@ -797,7 +819,7 @@ vgc_status backward_as(const void *x, const void *dy, const float *gamma, const 
         const auto fn = norm_backward<T, kVec, kParts, decltype(mode)::value, decltype(wide)::value>;
         constexpr int kOwn = kParts > 1 && decltype(mode)::value == kRows ? 64 * kParts : 0;      // bytes a thread: its sums of squares
         static_assert(R::smem(kBlock) + kOwn * kBlock + 16384 <= 232448, "");
-        if (R::kRing || kOwn) VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock) + kOwn * kBlock));
+        VGC_CUDA_OK(allow_dynamic_smem(reinterpret_cast<const void *>(fn), R::smem(kBlock) + kOwn * kBlock));
         VGC_CUDA_OK(launch_kernel(fn, dim3((unsigned)plan.blocks, plan.wide ? (unsigned)((features + kSeg - 1) / kSeg) : 1u), dim3((unsigned)threads),
                                   R::smem(threads) + kOwn * threads, st, true, p));
         count_launch();

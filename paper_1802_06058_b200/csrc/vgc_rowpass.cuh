@@ -11,13 +11,13 @@ namespace vgc {
 constexpr int kSeg = 256;           // features of a row that one warp takes: 8 per lane
 constexpr int kMaxRows = 2147483647 - 128;
 
-// Which features lane `lane` holds of a segment.  kVec (rows start on 16 bytes): 16-byte pieces, bf16 8 * lane + i, fp32
-// 128 * (i / 4) + 4 * lane + i % 4.  Otherwise single elements, neighbouring lanes next to one another: 32 * i + lane.
+// Which features lane `lane` holds of a segment: 16-byte pieces, bf16 8 * lane + i, fp32 128 * (i / 4) + 4 * lane + i % 4.  Where fp32 rows
+// do not start on 16 bytes (kVec false): single elements, neighbouring lanes next to one another, 32 * i + lane.
 template <class T, bool kVec>
 __device__ __forceinline__ int seg_col(int i, int lane)
 {
-    if (!kVec) return 32 * i + lane;
-    return sizeof(T) == 2 ? 8 * lane + i : 128 * (i >> 2) + 4 * lane + (i & 3);
+    if (sizeof(T) == 2) return 8 * lane + i;
+    return kVec ? 128 * (i >> 2) + 4 * lane + (i & 3) : 32 * i + lane;
 }
 
 // a lane's 8 features of a segment as they lie in memory
@@ -48,6 +48,47 @@ __device__ __forceinline__ void st_16(void *p, uint4 v)
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
+// ---- bf16 rows that do not start on 16 bytes: aligned pieces, shifted between neighbouring lanes --------------------------------------
+// 16 bytes from byte `off` (even, below 16, the same in the whole warp) of the 32 bytes lo, hi
+__device__ __forceinline__ uint4 bytes_from(uint4 lo, uint4 hi, uint32_t off)
+{
+    const bool two = off & 8, one = off & 4, half = off & 2;
+    const uint32_t a0 = two ? lo.z : lo.x, a1 = two ? lo.w : lo.y, a2 = two ? hi.x : lo.z, a3 = two ? hi.y : lo.w, a4 = two ? hi.z : hi.x, a5 = two ? hi.w : hi.y;
+    const uint32_t b0 = one ? a1 : a0, b1 = one ? a2 : a1, b2 = one ? a3 : a2, b3 = one ? a4 : a3, b4 = one ? a5 : a4;
+    const uint32_t bits = half ? 16 : 0;
+    return make_uint4(__funnelshift_r(b0, b1, bits), __funnelshift_r(b1, b2, bits), __funnelshift_r(b2, b3, bits), __funnelshift_r(b3, b4, bits));
+}
+__device__ __forceinline__ uint32_t word_of(uint4 v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+// 16 bytes from an aligned address on, zeros from `end` (even) on, where nothing is read
+__device__ __forceinline__ uint4 ld_16_until(uintptr_t at, uintptr_t end)
+{
+    if (at + 16 <= end) return ld_16(reinterpret_cast<const void *>(at));
+    uint32_t w[4] = {};
+    if (at < end) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (at + 2 * i < end) w[i >> 1] |= ld_h(reinterpret_cast<const uint16_t *>(at + 2 * i)) << (16 * (i & 1));
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Of 16 bytes for an aligned address those from byte `first` on (even, not 0), and those before byte `last` (even, not 0): in pieces of
+// 2, 4 and 8 bytes.
+__device__ __forceinline__ uint32_t word_of(uint4 v, uint32_t i) { return i & 2 ? (i & 1 ? v.w : v.z) : (i & 1 ? v.y : v.x); }
+__device__ __forceinline__ void st_head(char *at, uint4 v, uint32_t first)
+{
+    if (first & 2) *reinterpret_cast<uint16_t *>(at + first) = (uint16_t)(word_of(v, first >> 2) >> 16);
+    first = (first + 2) & ~3u;
+    if (first & 4) *reinterpret_cast<uint32_t *>(at + first) = word_of(v, first >> 2);
+    first = (first + 4) & ~7u;
+    if (first == 8) *reinterpret_cast<uint2 *>(at + 8) = make_uint2(v.z, v.w);
+}
+__device__ __forceinline__ void st_tail(char *at, uint4 v, uint32_t last)
+{
+    if (last & 8) *reinterpret_cast<uint2 *>(at) = make_uint2(v.x, v.y);
+    if (last & 4) *reinterpret_cast<uint32_t *>(at + (last & 8)) = last & 8 ? v.z : v.x;
+    if (last & 2) *reinterpret_cast<uint16_t *>(at + (last & 12)) = (uint16_t)word_of(v, last >> 2);
+}
+
 // `seg`: the segment's first feature's address; `left`: features of the row from there on.  What lies past the row's end is 0.
 template <bool kVec>
 __device__ __forceinline__ void load_seg(const float *seg, int left, int lane, Raw<float> &r)
@@ -72,12 +113,13 @@ __device__ __forceinline__ void load_seg(const __nv_bfloat16 *seg, int left, int
         const uint4 v = 8 * lane < left ? ld_16(seg + 8 * lane) : make_uint4(0, 0, 0, 0);
         r.v[0] = v.x; r.v[1] = v.y; r.v[2] = v.z; r.v[3] = v.w;
     } else {
-        const uint16_t *const p = reinterpret_cast<const uint16_t *>(seg) + lane;
-        uint32_t h[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = 32 * i + lane < left ? ld_h(p + 32 * i) : 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i] = h[2 * i] | h[2 * i + 1] << 16;
+        const uintptr_t at = reinterpret_cast<uintptr_t>(seg), off = at & 15, base = at - off, end = at + 2 * (left > 0 ? left : 0);
+        const uint4 own = ld_16_until(base + 16 * lane, end), past = lane == 31 && off ? ld_16_until(base + 512, end) : make_uint4(0, 0, 0, 0);
+        uint4 next;
+        next.x = __shfl_down_sync(~0u, own.x, 1); next.y = __shfl_down_sync(~0u, own.y, 1);
+        next.z = __shfl_down_sync(~0u, own.z, 1); next.w = __shfl_down_sync(~0u, own.w, 1);
+        const uint4 v = bytes_from(own, lane == 31 ? past : next, (uint32_t)off);
+        r.v[0] = v.x; r.v[1] = v.y; r.v[2] = v.z; r.v[3] = v.w;
     }
 }
 __device__ __forceinline__ float value(const Raw<float> &r, int i) { return r.v[i]; }
@@ -127,10 +169,26 @@ __device__ __forceinline__ void store_seg(__nv_bfloat16 *seg, int left, int lane
     if constexpr (kVec) {
         if (8 * lane < left) st_16(seg + 8 * lane, make_uint4(r.v[0], r.v[1], r.v[2], r.v[3]));
     } else {
-        uint16_t *const p = reinterpret_cast<uint16_t *>(seg) + lane;
+        const uint32_t off = (uint32_t)reinterpret_cast<uintptr_t>(seg) & 15u;
+        char *const base = reinterpret_cast<char *>(seg) - off;
+        const int end = (int)off + 2 * (left < kSeg ? left > 0 ? left : 0 : kSeg), mine = 16 * lane;      // bytes from the first aligned piece
+        const uint4 own = make_uint4(r.v[0], r.v[1], r.v[2], r.v[3]);
+        uint4 before;
+        before.x = __shfl_up_sync(~0u, own.x, 1); before.y = __shfl_up_sync(~0u, own.y, 1);
+        before.z = __shfl_up_sync(~0u, own.z, 1); before.w = __shfl_up_sync(~0u, own.w, 1);
+        if (end < 16 && off) {                                // all within one piece: features 0 ... 6, in the first lane
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (32 * i + lane < left) p[32 * i] = (uint16_t)(r.v[i >> 1] >> (16 * (i & 1)));
+            for (int i = 0; i < 7; ++i)
+                if (lane == 0 && (int)off + 2 * i < end) *reinterpret_cast<uint16_t *>(base + off + 2 * i) = (uint16_t)(r.v[i >> 1] >> (16 * (i & 1)));
+            return;
+        }
+        const uint4 v = off ? bytes_from(before, own, 16 - off) : own;
+        const bool head = lane == 0 && off;                   // the piece that the segment before, or the row before, shares
+        if (!head && mine + 16 <= end) st_16(base + mine, v);
+        if (head) st_head(base, v, off);
+        const bool past = end >= 512;                         // behind the last lane's piece there is a 33rd
+        const uint32_t last = past ? (uint32_t)end - 512u : (uint32_t)end & 15u;
+        if (last && !head && lane == (past ? 31 : end >> 4)) st_tail(base + (past ? 512 : mine), past ? bytes_from(own, own, 16 - off) : v, last);
     }
 }
 
@@ -293,7 +351,7 @@ __device__ __forceinline__ void store_blocks(const Checkpoint &c, int row, int f
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = infinity_to_nan(v[j]);
     }
-    if constexpr (kVec && sizeof(T) == 2) {               // a block is four lanes, 128 features sixteen
+    if constexpr (sizeof(T) == 2) {                       // a block is four lanes, 128 features sixteen
         uint32_t m = __float_as_uint(most(0, 4));
         m = max(m, __shfl_xor_sync(~0u, m, 1));
         m = max(m, __shfl_xor_sync(~0u, m, 2));
