@@ -185,6 +185,35 @@ struct Rows {
     }
 };
 
+// Four neighbouring features' gain or bias from feature c on, of C; `v` null: `otherwise` everywhere, as past the end.  `wide`: v is on 16
+// bytes (c is a multiple of four).
+__device__ __forceinline__ void four_of(const float *v, int c, int C, float otherwise, bool wide, F2 &a, F2 &b)
+{
+    if (wide && v && c + 4 <= C) {
+        const uint4 u = ld_16(v + c);
+        a = f2(__uint_as_float(u.x), __uint_as_float(u.y));
+        b = f2(__uint_as_float(u.z), __uint_as_float(u.w));
+    } else {
+        a = f2(v && c < C ? ld_f(v + c) : otherwise, v && c + 1 < C ? ld_f(v + c + 1) : otherwise);
+        b = f2(v && c + 2 < C ? ld_f(v + c + 2) : otherwise, v && c + 3 < C ? ld_f(v + c + 3) : otherwise);
+    }
+}
+// a lane's eight of a segment that begins with feature `first`
+template <class T, bool kVec>
+__device__ __forceinline__ void eight_of(const float *v, int first, int C, float otherwise, bool wide, int lane, F2 (&out)[4])
+{
+    if constexpr (kVec || sizeof(T) == 2) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) four_of(v, first + seg_col<T, kVec>(4 * h, lane), C, otherwise, wide, out[2 * h], out[2 * h + 1]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int c0 = first + seg_col<T, kVec>(2 * j, lane), c1 = first + seg_col<T, kVec>(2 * j + 1, lane);
+            out[j] = f2(v && c0 < C ? ld_f(v + c0) : otherwise, v && c1 < C ? ld_f(v + c1) : otherwise);
+        }
+    }
+}
+
 // ---- forward ------------------------------------------------------------------------------------------------------------------
 template <class T>
 struct Forward {
@@ -194,7 +223,7 @@ struct Forward {
     float *mean, *rstd;
     int rows, features, warps, groups;      // warps of a row, groups of warps a block
     float eps;
-    bool vectors;                           // gain and bias both there and on 16 bytes
+    bool gamma_wide, beta_wide;             // on 16 bytes
     Checkpoint c;
 };
 
@@ -214,18 +243,12 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
     const bool full = first + kParts * kSeg <= C;
     constexpr bool kKept = kParts <= 2;      // gain and bias in registers
     F2 gain[kKept ? kParts : 1][4], bias[kKept ? kParts : 1][4];
-    auto vector = [&](const float *v, int at, int j, float otherwise) {
-        const int c0 = at + seg_col<T, kVec>(2 * j, lane), c1 = at + seg_col<T, kVec>(2 * j + 1, lane);
-        return f2(v && c0 < C ? ld_f(v + c0) : otherwise, v && c1 < C ? ld_f(v + c1) : otherwise);
-    };
     if constexpr (kKept) {
 #pragma unroll
-        for (int k = 0; k < kParts; ++k)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                gain[k][j] = vector(p.gamma, first + k * kSeg, j, 1.f);
-                bias[k][j] = vector(p.beta, first + k * kSeg, j, 0.f);
-            }
+        for (int k = 0; k < kParts; ++k) {
+            eight_of<T, kVec>(p.gamma, first + k * kSeg, C, 1.f, p.gamma_wide, lane, gain[k]);
+            eight_of<T, kVec>(p.beta, first + k * kSeg, C, 0.f, p.beta_wide, lane, bias[k]);
+        }
     }
     if (kCheckpoint && blockIdx.x == gridDim.x - 1) clear_row_padding(p.c, p.rows, threadIdx.x, blockDim.x);
     const float per = 1.f / (float)C;
@@ -307,7 +330,7 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
                         g[j] = gain[kKept ? k : 0][j];
                         b[j] = bias[kKept ? k : 0][j];
                     }
-                } else if (kVec && full && p.vectors) {
+                } else if (kVec && full && p.gamma && p.beta && p.gamma_wide && p.beta_wide) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {             // four neighbouring features
                         const int at = c + seg_col<T, kVec>(4 * h, lane);
@@ -318,11 +341,8 @@ __global__ void __launch_bounds__(kBlock, 1) norm_forward(const Forward<T> p)
                         b[2 * h + 1] = f2(__uint_as_float(w.z), __uint_as_float(w.w));
                     }
                 } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        g[j] = vector(p.gamma, c, j, 1.f);
-                        b[j] = vector(p.beta, c, j, 0.f);
-                    }
+                    eight_of<T, kVec>(p.gamma, c, C, 1.f, false, lane, g);
+                    eight_of<T, kVec>(p.beta, c, C, 0.f, false, lane, b);
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -354,7 +374,7 @@ vgc_status forward_as(const void *x, const float *gamma, const float *beta, int 
     p.y = static_cast<T *>(y);
     p.gamma = gamma; p.beta = beta; p.mean = mean; p.rstd = rstd;
     p.rows = rows; p.features = features; p.eps = eps;
-    p.vectors = gamma && beta && aligned16(gamma) && aligned16(beta);
+    p.gamma_wide = aligned16(gamma); p.beta_wide = aligned16(beta);
     p.c = {};
     if (checkpoint) p.c = checkpoint_at(checkpoint, rows, features);
     // (16384 x 4096 with the checkpoint: bf16 88 us with 16 features a lane and 102 with 8; fp32, short of registers, 150 and 127)
