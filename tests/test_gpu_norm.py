@@ -297,3 +297,20 @@ def test_no_rows_and_refusals():
     with pytest.raises(vgc.VgcError) as err:
         vgc.vgc_layernorm(wide, None, None, EPS, wide, m, m)
     assert err.value.status == 2
+
+
+@pytest.mark.parametrize("rows,features", [(700, 1001), (50, 257), (3, 7), (90, 4099)])
+def test_in_place_rows_off_16_bytes(rows, features):
+    """bf16 rows that share 16-byte pieces with their neighbours: y over x, dx over dy, dx over x, for many rows in flight."""
+    x, dy = activations(rows, features, torch.bfloat16, 1), errors(rows, features, torch.bfloat16, 2)
+    gamma, beta = vectors(features, 5)
+    want, mean, rstd, _ = forward(x, gamma, beta)
+    z, m, r = x.clone(), torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    vgc.vgc_layernorm(z, gamma, beta, EPS, z, m, r)
+    assert torch.equal(z, want) and torch.equal(m, mean) and torch.equal(r, rstd)
+    want, sums = backward(x, dy, gamma, mean, rstd)
+    ws = workspace(vgc.vgc_layernorm_backward_workspace_bytes(rows, features, 1)).t
+    for over_dy in (True, False):
+        a, b, out = x.clone(), dy.clone(), [torch.empty(features, device="cuda") for _ in range(4)]
+        vgc.vgc_layernorm_backward(a, b, gamma, mean, rstd, b if over_dy else a, *out, ws=ws)
+        assert torch.equal(b if over_dy else a, want) and all(torch.equal(p, q) for p, q in zip(out, sums))
