@@ -4,8 +4,9 @@
 // row (one 16-byte load a lane in bf16), finds the blocks' maxima with two or three shuffles, and has kFlight such segments
 // in flight.  Power-of-two scales make the scaling exact, so that the code's own rounding is the only one.
 // Measured (B200, of the measured copy rate): 16384 x 16384 bf16 store 147 us (0.86), load 156 us (0.81); 16384 x 4096 fp32 58 us (0.90) and
-// 61 us (0.85).  Rows that do not start on 16 bytes go by single elements: 30000 x 1001 bf16 46 and 38 us (0.31, 0.37), fp32 40 and
-// 45 us (0.58, 0.52).  (With a 64-bit division for every segment and maxima on integers the store took 196 us.)
+// 61 us (0.85).  Rows that do not start on 16 bytes, 30000 x 1001: bf16, in aligned pieces shifted between lanes, 32 and 30 us (0.44, 0.47;
+// by single elements 46 and 38); fp32, by single elements, 40 and 45 us (0.58, 0.52).  (With a 64-bit division for every segment and
+// maxima on integers the store of 16384 x 16384 took 196 us.)
 #include "vgc_rowpass.cuh"
 
 namespace vgc {
